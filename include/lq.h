@@ -571,6 +571,114 @@ int lq_order_groups(int32_t n_group_cols, const int32_t* group_card, int32_t n_m
                     const int64_t* sums, const int64_t* counts, int32_t n_keys,
                     const lq_sort_key* keys, int32_t* order, int32_t* n_out, void* hip_stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Grouped operators: a key chooses the MODEL of a row.  In the calls above a key chooses a row of a
+ * dimension table; here it chooses one of G matrices of one shape: a model per store or segment, an
+ * expert per token, a low-rank adapter per request.  With the indicator matrix I of the keys
+ * (I[i][g] = 1 where row i belongs to group g; a row without a group has an empty row in I):
+ *   product   y_i  = sum_g I[i][g] (x_i W_g + b_g)
+ *   gradient  dW_g = sum_i I[i][g] x_i^T dy_i,   db_g = sum_i I[i][g] dy_i
+ *   adapter   y_i  = x_i W + b + sum_g I[i][g] scale_g (x_i A_g) B_g
+ * I is stored as the row numbers of group 0, of group 1, ... side by side (lq_group_rows), which a
+ * program makes once per batch and uses for every layer, forward and backward.
+ * Sums are fp32 whatever the element type.  They are taken in an order that depends on the sizes of
+ * the call, of the groups and on alignment, never on timing: the same call gives the same bits.
+ * ------------------------------------------------------------------------------------- */
+#define LQ_MAX_MODELS 4096   /* most groups */
+#define LQ_MAX_RANK 256      /* widest low-rank factor */
+
+/* `count` row-major matrices of one shape on the device, `stride` elements apart. */
+typedef struct {
+  void*   data;   /* device; may be NULL only when count*rows*cols == 0 */
+  int32_t count;
+  int32_t rows;
+  int32_t cols;
+  int32_t dtype;  /* lq_dtype */
+  int64_t ld;     /* elements between consecutive rows, >= cols */
+  int64_t stride; /* elements between consecutive matrices (0: all the same one; inputs only) */
+} lq_stack;
+
+/* Which rows belong to which group.  Position p, for offsets[g] <= p < offsets[g + 1], holds row
+ * order[p] of group g; positions from offsets[n_groups] to n hold the rows without a group. */
+typedef struct {
+  int64_t        n;        /* positions, < 2^31 */
+  int32_t        n_groups; /* 1..LQ_MAX_MODELS */
+  const int32_t* offsets;  /* device, [n_groups + 1], ascending, offsets[0] = 0, last one <= n */
+  const int32_t* order;    /* device, [n], each value of 0 .. n - 1 once; NULL: order[p] = p */
+} lq_groups;
+
+/* flags of the grouped calls */
+#define LQ_RELU 0x10u       /* lq_grouped_product: y = max(y, 0) */
+#define LQ_TRANSPOSED 0x20u /* lq_grouped_product: W_g^T instead of W_g */
+#define LQ_X_GROUPED 0x40u  /* row p of X belongs to position p, not to row order[p] */
+#define LQ_Y_GROUPED 0x80u  /* likewise rows of Y (dY) and of gate */
+
+/*
+ * Groups rows by key: a stable counting sort.
+ *   keys     device int32 [n]; a key outside [0, n_groups) means "no group" (a mapped key of -1 drops
+ *            out of an inner join the same way), unless LQ_CHECK_FKS is set: a key >= n_groups is
+ *            then LQ_ERR_FK_RANGE and the outputs stay untouched (the call waits for that check)
+ *   offsets  device int32 [n_groups + 1], out
+ *   order    device int32 [n], out: rows of group 0 in ascending order, of group 1, ..., then the rows
+ *            without a group, ascending
+ *   ws       lq_group_rows_workspace_bytes(n, n_groups) bytes, 256-byte aligned (NULL where that is 0;
+ *            LQ_CHECK_FKS needs 256 bytes at least)
+ */
+int lq_group_rows(const int32_t* keys, int64_t n, int32_t n_groups, int32_t* offsets, int32_t* order,
+                  void* ws, size_t ws_bytes, uint32_t flags, void* hip_stream);
+size_t lq_group_rows_workspace_bytes(int64_t n, int32_t n_groups);
+
+/*
+ * Product with the matrix of the row's group.  With r = order[p] for every position p of group g:
+ *   Y[r] = act(X[r / x_slots] W_g + bias_g)                 (act: ReLU with LQ_RELU)
+ *   Y[r] = 0 for the rows without a group
+ * Rows of Y that order does not name are left as they are.
+ *   X      [n / x_slots x k].  x_slots > 1: row i of X stands for the rows i * x_slots ..
+ *          i * x_slots + x_slots - 1 of Y, which may belong to different groups (a row routed to
+ *          several experts); with LQ_X_GROUPED x_slots must be 1
+ *   W      n_groups matrices [k x l] of X's type
+ *   bias   NULL or [n_groups x l] of X's type
+ *   gate   NULL or a matrix shaped like Y: results are zero where gate is not > 0 (a NaN is not)
+ *   Y      [n x l], of X's type (or f32 when that is bf16); must not overlap an input
+ * LQ_TRANSPOSED: X is [n x l] and Y [n x k], Y[r] = X[r] W_g^T: the gradient of the forward call's X from that of
+ * its Y, with `gate` = that X where a ReLU made it.  (x_slots must be 1: a program adds up the slots.)
+ *   ws     256-byte aligned, lq_grouped_workspace_bytes(..) bytes; a smaller one (or NULL) is allowed and may run slower
+ *          (LQ_CHECK_FKS needs 256 bytes: offsets and order are then verified first, the call waits for that, and
+ *          LQ_ERR_FK_RANGE leaves Y untouched)
+ */
+int lq_grouped_product(const lq_groups* groups, const lq_mat* X, int32_t x_slots, const lq_stack* W,
+                       const lq_mat* bias, const lq_mat* gate, lq_mat* Y, void* ws, size_t ws_bytes,
+                       uint32_t flags, void* hip_stream);
+
+/*
+ * Gradients of W and bias of lq_grouped_product, from its X and the gradient dY of its Y (before the ReLU):
+ *   dW_g = sum of X[r / x_slots]^T dY[r] over the rows r of group g,   db_g = sum of dY[r]
+ * Zeros for a group without rows.
+ *   X, dY  as X and Y above, of one type
+ *   dW     n_groups matrices [k x l], of X's type or f32, overwritten;  db  NULL or [n_groups x l] of dW's type
+ *   flags  LQ_X_GROUPED, LQ_Y_GROUPED, LQ_CHECK_FKS;  ws as above
+ */
+int lq_grouped_gradient(const lq_groups* groups, const lq_mat* X, int32_t x_slots, const lq_mat* dY,
+                        lq_stack* dW, lq_mat* db, void* ws, size_t ws_bytes, uint32_t flags, void* hip_stream);
+
+/* Workspace with which the two calls above run fastest: k, l, dtype of the matrices (0: none is needed). */
+size_t lq_grouped_workspace_bytes(int64_t n, int32_t n_groups, int32_t k, int32_t l, int32_t dtype);
+size_t lq_grouped_gradient_workspace_bytes(int64_t n, int32_t n_groups, int32_t k, int32_t l, int32_t dtype);
+
+/*
+ * One shared matrix and a low-rank adapter per group: with r = order[p] for every position p of group g,
+ *   Y[r] = X[r] W + bias + scale_g (X[r] A_g) B_g,  and  Y[r] = X[r] W + bias  for the rows without a group.
+ *   X [n x k], W [k x l], A n_groups matrices [k x rank], B n_groups matrices [rank x l], all of one type;
+ *   rank 1..LQ_MAX_RANK;  bias NULL or [1 x l] of that type;  scale device fp32 [n_groups] or NULL (all 1)
+ *   Y [n x l], of that type (or f32 when that is bf16); must not overlap an input
+ *   The products X A_g are kept in fp32.
+ *   flags  0 or LQ_CHECK_FKS;  ws  lq_adapter_workspace_bytes(..) bytes, 256-byte aligned, required
+ */
+int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W, const lq_mat* bias,
+                       const lq_stack* A, const lq_stack* B, const float* scale, lq_mat* Y, void* ws,
+                       size_t ws_bytes, uint32_t flags, void* hip_stream);
+size_t lq_adapter_workspace_bytes(int64_t n, int32_t n_groups, int32_t k, int32_t l, int32_t rank, int32_t dtype);
+
 /*
  * Plain device-to-device copy of `bytes` bytes (16-byte aligned pointers, bytes a
  * multiple of 16) by a grid-stride kernel.  Not part of the method: it is the

@@ -14,5 +14,7 @@ from .binding import (  # noqa: F401
     lq_keymap_lookup, lq_compact_matches, lq_project_dim_rows, lq_fusion_advice, lq_groupby_agg,
     lq_keymap64_bytes, lq_keymap64_build, lq_keymap64_insert, lq_keymap64_lookup,
     lq_masked_groupby_sum_static, lq_static_scratch_bytes, lq_group_avg, lq_yardstick_read, lq_yardstick_stream, lq_yardstick_gather, lq_yardstick_matrix,
+    lq_group_rows, lq_group_rows_workspace_bytes, lq_grouped_product, lq_grouped_workspace_bytes, lq_grouped_gradient,
+    lq_grouped_gradient_workspace_bytes, lq_adapter_product, lq_adapter_workspace_bytes, LQ_MAX_MODELS, LQ_MAX_RANK,
     lq_group_domain, lq_group_domain_workspace_bytes, lq_order_groups, LQ_KEY_GROUP_COLUMN, LQ_KEY_SUM, LQ_KEY_COUNT,
 )

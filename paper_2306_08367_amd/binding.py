@@ -26,6 +26,8 @@ LQ_F32, LQ_BF16 = 0, 1
 LQ_CHECK_KEYS = 2
 LQ_REUSE_SIDE_TABLES = 4
 LQ_KEY_GROUP_COLUMN, LQ_KEY_SUM, LQ_KEY_COUNT = 0, 1, 2
+LQ_RELU, LQ_TRANSPOSED, LQ_X_GROUPED, LQ_Y_GROUPED = 0x10, 0x20, 0x40, 0x80
+LQ_MAX_MODELS, LQ_MAX_RANK = 4096, 256
 _STATUS = {8: "LQ_ERR_DUPLICATE_KEY", 1: "LQ_ERR_NULL", 2: "LQ_ERR_SHAPE", 3: "LQ_ERR_DTYPE", 4: "LQ_ERR_WORKSPACE",
            5: "LQ_ERR_FK_RANGE", 6: "LQ_ERR_UNSUPPORTED", 7: "LQ_ERR_HIP"}
 
@@ -69,6 +71,15 @@ class lq_advice(ctypes.Structure):
 class lq_tree(ctypes.Structure):
     _fields_ = [("n_nodes", ctypes.c_int32), ("n_leaves", ctypes.c_int32), ("feature", ctypes.c_void_p),
                 ("threshold", ctypes.c_void_p), ("H", ctypes.c_void_p)]
+
+
+class lq_stack(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("count", ctypes.c_int32), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("ld", ctypes.c_int64), ("stride", ctypes.c_int64)]
+
+
+class lq_groups(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("n_groups", ctypes.c_int32), ("offsets", ctypes.c_void_p), ("order", ctypes.c_void_p)]
 
 
 class lq_model(ctypes.Structure):
@@ -172,6 +183,19 @@ def _load():
     lib.lq_fused_join_tree_masks.restype = ctypes.c_int
     lib.lq_tree_workspace_bytes.argtypes = [ps, pt, i64]
     lib.lq_tree_workspace_bytes.restype = sz
+    pg, pk = ctypes.POINTER(lq_groups), ctypes.POINTER(lq_stack)
+    lib.lq_group_rows.argtypes = [vp, i64, i32, vp, vp, vp, sz, u32, vp]
+    lib.lq_group_rows_workspace_bytes.argtypes = [i64, i32]
+    lib.lq_grouped_product.argtypes = [pg, pm, i32, pk, pm, pm, pm, vp, sz, u32, vp]
+    lib.lq_grouped_gradient.argtypes = [pg, pm, i32, pm, pk, pm, vp, sz, u32, vp]
+    lib.lq_grouped_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+    lib.lq_grouped_gradient_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+    lib.lq_adapter_product.argtypes = [pg, pm, pm, pm, pk, pk, vp, pm, vp, sz, u32, vp]
+    lib.lq_adapter_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32]
+    for f in ("lq_group_rows", "lq_grouped_product", "lq_grouped_gradient", "lq_adapter_product"):
+        getattr(lib, f).restype = ctypes.c_int
+    for f in ("lq_group_rows", "lq_grouped", "lq_grouped_gradient", "lq_adapter"):
+        getattr(lib, f + "_workspace_bytes").restype = sz
     lib.lq_last_error.restype = ctypes.c_char_p
     lib.lq_version.restype = ctypes.c_char_p
     for f in ("lq_project_dims", "lq_fused_join_predict", "lq_materialized_join_predict",
@@ -698,3 +722,61 @@ def lq_groupby_agg(fks: Sequence[torch.Tensor], dim_rows: Sequence[int], dim_mas
         fks, dim_rows, dim_mask, dim_code, group_card, preds, [(_MEASURE_OPS[op], a, b) for op, a, b in measures],
         "sum" in want, "min" in want, "max" in want, "count" in want, ws, flags, stream)
     return {"sum": sums, "min": mins, "max": maxs, "count": counts}
+
+
+# ---------------------------------------------------------------- grouped operators ------------
+
+def lq_group_rows_workspace_bytes(n: int, n_groups: int) -> int:
+    return int(_lib.lq_group_rows_workspace_bytes(int(n), int(n_groups)))
+
+
+def lq_group_rows(keys: torch.Tensor, n_groups: int, offsets: Optional[torch.Tensor] = None, order: Optional[torch.Tensor] = None,
+                  flags: int = 0, ws: Optional[torch.Tensor] = None, stream=None):
+    """The rows of every group of a key column, a stable counting sort: (offsets int32 [n_groups + 1], order int32 [n]).
+    order[offsets[g] : offsets[g + 1]] are the rows whose key is g, ascending; rows whose key is no group (negative, or n_groups
+    and more unless LQ_CHECK_FKS refuses those) come last."""
+    return _lqpy.group_rows(keys, n_groups, offsets, order, flags, ws, stream)
+
+
+def lq_grouped_workspace_bytes(n: int, n_groups: int, k: int, l: int, dtype: int = LQ_F32) -> int:
+    return int(_lib.lq_grouped_workspace_bytes(int(n), int(n_groups), int(k), int(l), int(dtype)))
+
+
+def lq_grouped_product(X: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, order: Optional[torch.Tensor] = None,
+                       bias: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
+                       y_dtype: Optional[torch.dtype] = None, transposed: bool = False, relu: bool = False, x_grouped: bool = False,
+                       y_grouped: bool = False, x_slots: int = 1, flags: int = 0, ws: Optional[torch.Tensor] = None,
+                       stream=None) -> torch.Tensor:
+    """Y[r] = act(X[r // x_slots] W_g + bias_g) for every row r of group g; zeros for rows without a group.
+
+    W is [groups x k x l], bias [groups x l].  transposed: W_g^T, the gradient of X from that of Y; gate (shaped like Y): zero
+    where gate is not > 0, the ReLU behind which X came.  x_grouped / y_grouped: X / Y (and gate) hold row p at position p of
+    `order` instead of at order[p].  order None: the rows are in the order of the groups as they are."""
+    return _lqpy.grouped_product(X, W, offsets, order, bias, gate, Y, y_dtype, transposed, relu, x_grouped, y_grouped, x_slots, flags, ws,
+                                 stream)
+
+
+def lq_grouped_gradient_workspace_bytes(n: int, n_groups: int, k: int, l: int, dtype: int = LQ_F32) -> int:
+    return int(_lib.lq_grouped_gradient_workspace_bytes(int(n), int(n_groups), int(k), int(l), int(dtype)))
+
+
+def lq_grouped_gradient(X: torch.Tensor, dY: torch.Tensor, offsets: torch.Tensor, order: Optional[torch.Tensor] = None,
+                        dW: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None, dw_dtype: Optional[torch.dtype] = None,
+                        want_bias: bool = False, x_grouped: bool = False, y_grouped: bool = False, x_slots: int = 1, flags: int = 0,
+                        ws: Optional[torch.Tensor] = None, stream=None):
+    """(dW, db) of lq_grouped_product from its X and the gradient dY of its Y (before the ReLU): dW[g] = sum of
+    X[r // x_slots]^T dY[r] over the rows r of group g, db[g] = sum of dY[r] (None unless want_bias or db is given)."""
+    return _lqpy.grouped_gradient(X, dY, offsets, order, dW, db, dw_dtype, want_bias, x_grouped, y_grouped, x_slots, flags, ws, stream)
+
+
+def lq_adapter_workspace_bytes(n: int, n_groups: int, k: int, l: int, rank: int, dtype: int = LQ_F32) -> int:
+    return int(_lib.lq_adapter_workspace_bytes(int(n), int(n_groups), int(k), int(l), int(rank), int(dtype)))
+
+
+def lq_adapter_product(X: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.Tensor, offsets: torch.Tensor,
+                       order: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                       Y: Optional[torch.Tensor] = None, y_dtype: Optional[torch.dtype] = None, flags: int = 0,
+                       ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Y[r] = X[r] W + bias + scale[g] (X[r] A_g) B_g for every row r of group g; X[r] W + bias for rows without a group.
+    A is [groups x k x rank], B [groups x rank x l], scale fp32 [groups] (None: 1), bias [l]."""
+    return _lqpy.adapter_product(X, W, A, B, offsets, order, scale, bias, Y, y_dtype, flags, ws, stream)

@@ -1,0 +1,293 @@
+// Row numbers of every group from a column of keys: a stable counting sort by group.
+//
+// A workgroup takes a run of keys and each of its wavefronts a run of that.  Two passes over the keys: the first counts
+// the keys of every group per wavefront (LDS), the second puts every row at
+//   first place of the group + rows of earlier workgroups + of earlier wavefronts + of earlier lanes with the same key,
+// where the last term comes from comparing the 64 keys of a step bit by bit (ballots): no atomic decides a place, so the
+// order is the rows' own.  Few keys are done by one workgroup in one launch; more take three launches: counts per
+// workgroup, sums of those over the workgroups, places.
+// A key outside [0, G) counts as group G, whose rows come last.
+#include "grouped.h"
+
+namespace lq {
+namespace {
+
+constexpr int THREADS = 1024, WAVES = THREADS / 64;
+constexpr int64_t ONE_GROUP_KEYS = 16384;    // most keys of the one-workgroup form
+
+__device__ __forceinline__ int group_of_key(int key, int G) { return static_cast<unsigned>(key) < static_cast<unsigned>(G) ? key : G; }
+
+// Lanes of the wavefront whose key equals this lane's, among those of `active`.
+__device__ __forceinline__ unsigned long long same_key(int key, int bits, unsigned long long active) {
+  unsigned long long m = active;
+  for (int b = 0; b < bits; ++b) {
+    const bool one = (key >> b) & 1;
+    const unsigned long long v = __ballot(one);
+    m &= one ? v : ~v;
+  }
+  return m;
+}
+
+// Sum over the workgroup's threads below this one; *total: over all.
+__device__ __forceinline__ int scan_threads(int v, int* shared, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int upto = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int u = __shfl_up(upto, d);
+    if (lane >= d) upto += u;
+  }
+  if (lane == 63) shared[wave] = upto;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    before += w < wave ? shared[w] : 0;
+    all += shared[w];
+  }
+  __syncthreads();
+  *total = all;
+  return before + upto - v;
+}
+
+// LDS: base [G + 1] ints, then per wavefront [G + 1] 16-bit counts (a wavefront has fewer than 65,536 keys), padded to words.
+__host__ __device__ inline int count_words(int G) { return (G + 2) >> 1; }
+inline size_t place_lds(int G) { return (static_cast<size_t>(G) + 1 + static_cast<size_t>(WAVES) * count_words(G)) * 4; }
+
+// Keys [begin, end) of this workgroup, run [b, e) of a wavefront.
+__device__ __forceinline__ void wave_run(int64_t begin, int64_t end, int64_t* b, int64_t* e) {
+  const int64_t per = (end - begin + WAVES - 1) / WAVES;
+  const int wave = threadIdx.x >> 6;
+  *b = min(begin + wave * per, end);
+  *e = min(*b + per, end);
+}
+
+__device__ __forceinline__ void count_keys(const int32_t* __restrict__ keys, int G, int64_t b, int64_t e, unsigned int* mine) {
+  for (int64_t i = b + (threadIdx.x & 63); i < e; i += 64) {
+    const int g = group_of_key(keys[i], G);
+    atomicAdd(&mine[g >> 1], 1u << (16 * (g & 1)));
+  }
+}
+
+// Turns counts per wavefront into counts of the earlier wavefronts and calls total(g, sum) for every group.
+template <typename F> __device__ __forceinline__ void sum_waves(int G, unsigned short* counts, F&& total) {
+  const int stride = 2 * count_words(G);
+  for (int g = threadIdx.x; g <= G; g += THREADS) {
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const int v = counts[w * stride + g];
+      counts[w * stride + g] = static_cast<unsigned short>(sum);
+      sum += v;
+    }
+    total(g, sum);
+  }
+}
+
+__device__ __forceinline__ void place_rows(const int32_t* __restrict__ keys, int G, int bits, int64_t b, int64_t e, const int* base,
+                                           unsigned short* mine, int32_t* __restrict__ order) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t i0 = b; i0 < e; i0 += 64) {
+    const int64_t i = i0 + lane;
+    const bool in = i < e;
+    const int g = in ? group_of_key(keys[i], G) : 0;
+    const unsigned long long same = same_key(g, bits, __ballot(in));
+    if (in) {
+      const int earlier = __popcll(same & ((1ull << lane) - 1));
+      const int before = mine[g];
+      order[base[g] + before + earlier] = static_cast<int32_t>(i);
+      if (earlier == 0) mine[g] = static_cast<unsigned short>(before + __popcll(same));
+    }
+    __builtin_amdgcn_wave_barrier();     // (the next step's lanes read what this one's wrote: LDS keeps a wavefront's order)
+  }
+}
+
+__global__ __launch_bounds__(THREADS) void group_rows_kernel(const int32_t* __restrict__ keys, int n, int G, int bits,
+                                                             int32_t* __restrict__ off, int32_t* __restrict__ order) {
+  extern __shared__ int shared_base[];
+  __shared__ int waves[WAVES];
+  unsigned int* counts = reinterpret_cast<unsigned int*>(shared_base + G + 1);
+  const int words = count_words(G);
+  for (int i = threadIdx.x; i < WAVES * words; i += THREADS) counts[i] = 0;
+  __syncthreads();
+  int64_t b, e;
+  wave_run(0, n, &b, &e);
+  unsigned int* mine = counts + (threadIdx.x >> 6) * words;
+  count_keys(keys, G, b, e, mine);
+  __syncthreads();
+  sum_waves(G, reinterpret_cast<unsigned short*>(counts), [&](int g, int sum) { shared_base[g] = sum; });
+  __syncthreads();
+  int first = 0;
+  for (int g0 = 0; g0 <= G; g0 += THREADS) {
+    const int g = g0 + threadIdx.x;
+    int total;
+    const int before = scan_threads(g <= G ? shared_base[g] : 0, waves, &total);
+    if (g <= G) {
+      shared_base[g] = first + before;
+      off[g] = first + before;
+    }
+    first += total;
+  }
+  __syncthreads();
+  place_rows(keys, G, bits, b, e, shared_base, reinterpret_cast<unsigned short*>(mine), order);
+}
+
+__global__ __launch_bounds__(THREADS) void group_count_kernel(const int32_t* __restrict__ keys, int64_t n, int64_t per, int G,
+                                                              int32_t* __restrict__ counts) {
+  extern __shared__ int hist[];
+  for (int g = threadIdx.x; g <= G; g += THREADS) hist[g] = 0;
+  __syncthreads();
+  const int64_t begin = blockIdx.x * per, end = min(begin + per, n);
+  for (int64_t i = begin + threadIdx.x; i < end; i += THREADS) atomicAdd(&hist[group_of_key(keys[i], G)], 1);
+  __syncthreads();
+  for (int g = threadIdx.x; g <= G; g += THREADS) counts[static_cast<int64_t>(blockIdx.x) * (G + 1) + g] = hist[g];
+}
+
+// counts[b][g] becomes the rows of group g in workgroups before b; totals[g] all of them.  64 groups a workgroup, the
+// workgroups' counts in 16 parts.
+__global__ __launch_bounds__(THREADS) void group_sum_kernel(int blocks, int G, int32_t* __restrict__ counts, int32_t* __restrict__ totals) {
+  __shared__ int part[WAVES][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = blockIdx.x * 64 + lane;
+  const int per = (blocks + WAVES - 1) / WAVES, b0 = min(wave * per, blocks), b1 = min(b0 + per, blocks);
+  int sum = 0;
+  if (g <= G)
+    for (int b = b0; b < b1; ++b) sum += counts[static_cast<int64_t>(b) * (G + 1) + g];
+  part[wave][lane] = sum;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    before += w < wave ? part[w][lane] : 0;
+    all += part[w][lane];
+  }
+  if (g > G) return;
+  for (int b = b0; b < b1; ++b) {
+    const int64_t at = static_cast<int64_t>(b) * (G + 1) + g;
+    const int v = counts[at];
+    counts[at] = before;
+    before += v;
+  }
+  if (wave == 0) totals[g] = all;
+}
+
+__global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __restrict__ keys, int64_t n, int64_t per, int G, int bits,
+                                                              const int32_t* __restrict__ counts, const int32_t* __restrict__ totals,
+                                                              int32_t* __restrict__ off, int32_t* __restrict__ order) {
+  extern __shared__ int shared_base[];
+  __shared__ int waves[WAVES];
+  unsigned int* own = reinterpret_cast<unsigned int*>(shared_base + G + 1);
+  const int words = count_words(G);
+  for (int i = threadIdx.x; i < WAVES * words; i += THREADS) own[i] = 0;
+  __syncthreads();
+  const int64_t begin = blockIdx.x * per, end = min(begin + per, n);
+  int64_t b, e;
+  wave_run(begin, max(begin, end), &b, &e);
+  unsigned int* mine = own + (threadIdx.x >> 6) * words;
+  count_keys(keys, G, b, e, mine);
+  int first = 0;
+  for (int g0 = 0; g0 <= G; g0 += THREADS) {
+    const int g = g0 + threadIdx.x;
+    int total;
+    const int before = scan_threads(g <= G ? totals[g] : 0, waves, &total);
+    if (g <= G) {
+      shared_base[g] = first + before + counts[static_cast<int64_t>(blockIdx.x) * (G + 1) + g];
+      if (blockIdx.x == 0) off[g] = first + before;
+    }
+    first += total;
+  }
+  __syncthreads();
+  sum_waves(G, reinterpret_cast<unsigned short*>(own), [](int, int) {});
+  __syncthreads();
+  place_rows(keys, G, bits, b, e, shared_base, reinterpret_cast<unsigned short*>(mine), order);
+}
+
+// Keys and number of workgroups of the three-launch form: 256 workgroups (one a compute unit) unless that leaves them fewer
+// than 4,096 keys, and at most 512K keys each (16-bit counts per wavefront hold 65,535).
+void split(int64_t n, int64_t* per, int* blocks) {
+  int64_t p = std::max<int64_t>(4096, (n + 255) / 256);
+  p = std::min<int64_t>((p + 1023) / 1024 * 1024, 1 << 19);
+  *per = p;
+  *blocks = static_cast<int>((n + p - 1) / p);
+}
+
+// Marks bit 0 where a key is G or more.
+__global__ void check_keys_kernel(const int32_t* __restrict__ keys, int64_t n, int G, int32_t* flag) {
+  bool bad = false;
+  for (int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * blockDim.x)
+    bad |= keys[i] >= G;
+  if (bad) atomicOr(flag, 1);
+}
+
+// Marks bit 0 where the offsets do not ascend from 0 to at most n, and bit 1 where an entry of order is outside [0, n).
+__global__ void check_groups_kernel(lq_groups g, int32_t* flag) {
+  const int64_t i0 = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x, step = static_cast<int64_t>(gridDim.x) * blockDim.x;
+  int bad = 0;
+  for (int64_t i = i0; i <= g.n_groups; i += step) {
+    const int v = g.offsets[i];
+    if (v > g.n || (i == 0 ? v != 0 : v < g.offsets[i - 1])) bad |= 1;
+  }
+  if (g.order)
+    for (int64_t i = i0; i < g.n; i += step)
+      if (static_cast<uint32_t>(g.order[i]) >= static_cast<uint64_t>(g.n)) bad |= 2;
+  if (bad) atomicOr(flag, bad);
+}
+__global__ void clear_flag_kernel(int32_t* flag) { *flag = 0; }
+
+}  // namespace
+
+size_t group_rows_ws_bytes(int64_t n, int32_t G) {
+  if (n <= ONE_GROUP_KEYS) return 0;
+  int64_t per;
+  int blocks;
+  split(n, &per, &blocks);
+  return round_up((static_cast<size_t>(blocks) + 1) * (G + 1) * 4, 256);
+}
+
+int launch_group_rows(const int32_t* keys, int64_t n, int32_t G, int32_t* off, int32_t* order, void* ws, hipStream_t s) {
+  int bits = 0;
+  while ((G >> bits) > 0) ++bits;
+  const size_t lds = place_lds(G);
+  if (n <= ONE_GROUP_KEYS) {
+    if (lds > 64 * 1024)
+      LQ_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&group_rows_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                     static_cast<int>(lds)));
+    group_rows_kernel<<<1, THREADS, lds, s>>>(keys, static_cast<int>(n), G, bits, off, order);
+    LQ_LAUNCH_CHECK("group_rows_kernel");
+    return LQ_OK;
+  }
+  int64_t per;
+  int blocks;
+  split(n, &per, &blocks);
+  int32_t* counts = static_cast<int32_t*>(ws);
+  int32_t* totals = counts + static_cast<int64_t>(blocks) * (G + 1);
+  group_count_kernel<<<blocks, THREADS, (G + 1) * 4, s>>>(keys, n, per, G, counts);
+  LQ_LAUNCH_CHECK("group_count_kernel");
+  group_sum_kernel<<<(G + 64) / 64, THREADS, 0, s>>>(blocks, G, counts, totals);
+  LQ_LAUNCH_CHECK("group_sum_kernel");
+  if (lds > 64 * 1024)
+    LQ_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&group_place_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                   static_cast<int>(lds)));
+  group_place_kernel<<<blocks, THREADS, lds, s>>>(keys, n, per, G, bits, counts, totals, off, order);
+  LQ_LAUNCH_CHECK("group_place_kernel");
+  return LQ_OK;
+}
+
+int launch_check_keys(const int32_t* keys, int64_t n, int32_t G, int32_t* flag, hipStream_t s) {
+  clear_flag_kernel<<<1, 1, 0, s>>>(flag);
+  LQ_LAUNCH_CHECK("clear_flag_kernel");
+  const int blocks = static_cast<int>(std::min<int64_t>((n + 255) / 256, 2048));
+  check_keys_kernel<<<std::max(blocks, 1), 256, 0, s>>>(keys, n, G, flag);
+  LQ_LAUNCH_CHECK("check_keys_kernel");
+  return LQ_OK;
+}
+
+int launch_check_groups(const lq_groups& g, int32_t* flag, hipStream_t s) {
+  clear_flag_kernel<<<1, 1, 0, s>>>(flag);
+  LQ_LAUNCH_CHECK("clear_flag_kernel");
+  const int blocks = static_cast<int>(std::min<int64_t>((std::max<int64_t>(g.n, g.n_groups) + 256) / 256, 2048));
+  check_groups_kernel<<<blocks, 256, 0, s>>>(g, flag);
+  LQ_LAUNCH_CHECK("check_groups_kernel");
+  return LQ_OK;
+}
+
+}  // namespace lq

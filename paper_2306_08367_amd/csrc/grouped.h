@@ -1,0 +1,235 @@
+// Shared by the kernels of the grouped operators (the matrix of a row is chosen by the row's group): descriptors,
+// the search of a workgroup for its tile, and the tile product that they are built from.
+#ifndef LQ_GROUPED_H_
+#define LQ_GROUPED_H_
+
+#include "lq_common.h"
+
+namespace lq {
+
+// Everything a product needs, by value as the kernel argument.  The operator is Y[row(p)] = X[row(p)] * W_group(p).
+struct GroupedArgs {
+  const int32_t* off;     // [G + 1]
+  const int32_t* order;   // [n] or NULL
+  int32_t G, n;
+  const void* X; int64_t ldx;
+  const void* W; int64_t ldw, sw;       // sw: elements from one matrix to the next
+  const void* bias; int64_t ldb;        // row g, or row 0 of a shared matrix
+  const void* gate; int64_t ldg;
+  void* Y; int64_t ldy;
+  int32_t K, N;           // inner width and width of the result
+  int32_t n_store;        // columns stored (>= N; those past N are zeros)
+  int32_t slots;          // row r of Y reads row r / slots of X
+  int32_t x_grouped, y_grouped;
+  int32_t relu, y_bf16;
+  int32_t y_vec;          // four results of a row may be loaded and stored together
+  int32_t tiles_n, row_tiles;
+  int32_t steps_per_split;   // K steps of one split; split z writes at Y + z * split_stride
+  int64_t split_stride;
+  int32_t* gpos;          // out: group of every position, -1 for none (or NULL)
+  // adapters: U [splits x n x rp] fp32 by position, B_g [rank x N]
+  const float* U; int64_t u_stride; int32_t u_splits, rp, rank;
+  const void* B; int64_t ldB, sB;
+  const float* scale;
+  const int32_t* group_of;   // gpos of the product that made U
+};
+
+struct GradientArgs {
+  const int32_t* off;
+  const int32_t* order;
+  int32_t G, n;
+  const void* X; int64_t ldx; int32_t slots, x_grouped;
+  const void* dY; int64_t ldy; int32_t y_grouped;
+  void* dW; int64_t ldw, sw; int32_t w_bf16, w_vec;
+  void* db; int64_t ldb;
+  int32_t k, l;
+  int32_t tiles_m, tiles_n;
+};
+
+int launch_group_rows(const int32_t* keys, int64_t n, int32_t G, int32_t* off, int32_t* order, void* ws, hipStream_t s);
+size_t group_rows_ws_bytes(int64_t n, int32_t G);
+int launch_check_groups(const lq_groups& g, int32_t* flag, hipStream_t s);
+int launch_check_keys(const int32_t* keys, int64_t n, int32_t G, int32_t* flag, hipStream_t s);
+// `in_vec`: rows of X and of the matrices may be read in aligned 16-byte pieces.
+int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed, bool in_vec, hipStream_t s);
+int launch_adapter_product(const GroupedArgs& main, const GroupedArgs& low, int32_t dtype, bool main_vec, bool low_vec, hipStream_t s);
+int launch_grouped_gradient(const GradientArgs& a, int32_t dtype, bool in_vec, hipStream_t s);
+
+#ifdef __HIPCC__
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
+
+// Sixteen bytes of zeros: what a lane reads where its operand has ended.
+static __device__ const u32x4 g_zeros = {0, 0, 0, 0};
+
+struct __attribute__((packed, aligned(2))) Bytes16 { unsigned int x, y, z, w; };
+
+// The 16 bytes at p, of which only the first `valid` elements exist (the others read as zero); any alignment.
+template <typename T> __device__ __forceinline__ u32x4 load_piece(const T* p, int valid) {
+  constexpr int PER = 16 / sizeof(T);
+  if (valid >= PER) {
+    const Bytes16 t = *reinterpret_cast<const Bytes16*>(p);
+    return u32x4{t.x, t.y, t.z, t.w};
+  }
+  u32x4 r = {0, 0, 0, 0};
+#pragma unroll
+  for (int q = 0; q < PER; ++q)
+    if (q < valid) {
+      if constexpr (sizeof(T) == 4) r[q] = reinterpret_cast<const unsigned int*>(p)[q];
+      else r[q >> 1] |= static_cast<unsigned int>(p[q]) << (16 * (q & 1));
+    }
+  return r;
+}
+
+// Position range and group of row tile t of TM rows: the tiles of group 0, of group 1, ..., then those of the rows
+// without a group (group -1).  rows == 0: there is no such tile.  Called by a whole wavefront: lane l adds up the
+// tiles of groups l * per .. l * per + per - 1, the sums are scanned over the lanes, and the lane that holds t walks
+// its groups again.
+struct RowTile { int group, first, rows; };
+template <int TM> __device__ __forceinline__ RowTile find_row_tile(const int32_t* __restrict__ off, int G, int n, int t) {
+  const int lane = threadIdx.x & 63;
+  const int per = (G + 63) >> 6;
+  const int g0 = min(lane * per, G), g1 = min(g0 + per, G);
+  int own = 0;
+  for (int g = g0; g < g1; ++g) own += (off[g + 1] - off[g] + TM - 1) / TM;
+  int upto = own;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(upto, d);
+    if (lane >= d) upto += v;
+  }
+  const int total = __shfl(upto, 63);
+  if (t >= total) {
+    const int first = off[G] + (t - total) * TM;
+    return {-1, first, max(0, min(TM, n - first))};
+  }
+  const unsigned long long holds = __ballot(upto > t);
+  const int at = __ffsll(static_cast<long long>(holds)) - 1;
+  int left = t - (upto - own), group = 0, first = 0, rows = 0;
+  if (lane == at) {
+    for (int g = g0; g < g1; ++g) {
+      const int b = off[g], e = off[g + 1], tiles = (e - b + TM - 1) / TM;
+      if (left < tiles) {
+        group = g;
+        first = b + left * TM;
+        rows = min(TM, e - first);
+        break;
+      }
+      left -= tiles;
+    }
+  }
+  return {__shfl(group, at), __shfl(first, at), __shfl(rows, at)};
+}
+
+// Workgroups go to the 8 dies in turn; each die gets a contiguous run of tiles, so that neighbouring tiles, which
+// share rows or a matrix, share an L2.
+__device__ __forceinline__ int die_order(int id, int total) {
+  const int per = total >> 3, more = total & 7, die = id & 7, at = id >> 3;
+  return die * per + min(die, more) + at;
+}
+
+// One operand of the tile product in LDS: EXT rows of the result (or columns) by KSTEP of the inner dimension, as
+// lines of 16-byte pieces.
+//   KMAJ    a line per row, the inner dimension along it (128 bytes): a lane's operand is one 16-byte read
+//   !KMAJ   a line per inner index, the rows along it: bf16 operands come transposed out of LDS
+//           (ds_read_b64_tr_b16: four inner indexes of a row a lane), fp32 ones a word at a time
+// Piece c of a line lies at place c ^ spread(line), so that the lanes of a read use all banks.
+template <typename T, bool KMAJ, int EXT, int THREADS> struct Operand {
+  static constexpr int EPC = 16 / sizeof(T);
+  static constexpr int KSTEP = 128 / sizeof(T);
+  static constexpr int LINES = KMAJ ? EXT : KSTEP;
+  static constexpr int CPL = KMAJ ? 8 : EXT / EPC;
+  static constexpr int PIECES = LINES * CPL;
+  static constexpr int PER = PIECES / THREADS;
+  static constexpr int BYTES = PIECES * 16;
+  static_assert(PIECES % THREADS == 0, "whole pieces a thread");
+
+  static __device__ __forceinline__ int spread(int line) {
+    if constexpr (KMAJ) return (line >> 1) & 7;
+    else if constexpr (sizeof(T) == 4) return 4 * ((line >> 2) & 3);
+    else if constexpr (CPL >= 16) return 2 * ((line & 3) | ((line >> 1) & 4));
+    else return 2 * (((line >> 1) & 1) | ((line >> 2) & 2));
+  }
+  static __device__ __forceinline__ int line_of(int i) { return (i * THREADS + static_cast<int>(threadIdx.x)) / CPL; }
+  // the piece of its line that thread's i-th place holds
+  static __device__ __forceinline__ int piece_of(int i) {
+    const int id = i * THREADS + threadIdx.x;
+    return (id % CPL) ^ spread(id / CPL);
+  }
+  static __device__ __forceinline__ int place(int line, int piece) { return (line * CPL + (piece ^ spread(line))) * 16; }
+
+  // Rows r0 .. r0 + 15 and inner block kk (32 of bf16, 16 of fp32) as a matrix-instruction operand.
+  static __device__ __forceinline__ u32x4 fragment(const char* lds, int r0, int kk) {
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    if constexpr (KMAJ) {
+      return *reinterpret_cast<const u32x4*>(lds + place(r0 + i, 4 * kk + g));
+    } else if constexpr (sizeof(T) == 2) {
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      const int k = 32 * kk + 8 * g + (i >> 2), c = (r0 >> 3) + ((i & 3) >> 1);
+      const char* p0 = lds + place(k, c) + 8 * (i & 1);
+      const char* p1 = lds + place(k + 4, c) + 8 * (i & 1);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p0);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p1);
+      const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+      return u32x4{a.x, a.y, b.x, b.y};
+    } else {
+      u32x4 r;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int k = 16 * kk + 4 * g + s, col = r0 + i;
+        r[s] = *reinterpret_cast<const unsigned int*>(lds + place(k, col >> 2) + 4 * (col & 3));
+      }
+      return r;
+    }
+  }
+};
+
+// acc[n][m] += sum over the block of b[n] a[m]: lane l holds row m = l % 16 and four neighbouring columns n = 4 (l / 16) ..
+// of the result.  fp32: the block of 16 in four instructions, each with the inner indexes 4 g + s.
+template <typename T> __device__ __forceinline__ f32x4 multiply(const u32x4& b, const u32x4& a, f32x4 acc) {
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, b), __builtin_bit_cast(bf16x8v, a), acc, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b[s]), __uint_as_float(a[s]), acc, 0, 0, 0);
+    return acc;
+  }
+}
+
+template <int TM_, int TN_, int WAVES_M_, int WAVES_N_> struct TileShape {
+  static constexpr int TM = TM_, TN = TN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_;
+  static constexpr int THREADS = 64 * WAVES_M * WAVES_N;
+  static constexpr int MI = TM / WAVES_M / 16, NI = TN / WAVES_N / 16;
+};
+
+// One step of the product of a wavefront's part of the tile.
+template <typename T, class S, class A, class B>
+__device__ __forceinline__ void multiply_step(const char* la, const char* lb, f32x4 (&acc)[S::MI][S::NI]) {
+  const int wave = threadIdx.x >> 6;
+  const int m0 = (wave / S::WAVES_N) * S::MI * 16, n0 = (wave % S::WAVES_N) * S::NI * 16;
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+    u32x4 a[S::MI], b[S::NI];
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) a[i] = A::fragment(la, m0 + 16 * i, kk);
+#pragma unroll
+    for (int j = 0; j < S::NI; ++j) b[j] = B::fragment(lb, n0 + 16 * j, kk);
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NI; ++j) acc[i][j] = multiply<T>(b[j], a[i], acc[i][j]);
+  }
+}
+
+// 16 bytes from memory straight into LDS: lane l's land at base + 16 l (`base` is the wavefront's).
+__device__ __forceinline__ void copy_to_lds(const void* p, char* base) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)base, 16, 0, 0);
+}
+
+#endif  // __HIPCC__
+}  // namespace lq
+#endif  // LQ_GROUPED_H_

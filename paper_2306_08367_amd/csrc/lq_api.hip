@@ -73,11 +73,9 @@ int launch_groupby_agg(int64_t n, int32_t K, const int32_t* const* fks, const in
 size_t groupby_tables_bytes(int32_t K, const int64_t* rows);
 int launch_group_avg(int32_t M, int64_t G, const int64_t* sums, const int64_t* counts, double* avgs, hipStream_t s);
 
-namespace {
-
 // What is wrong with a matrix that check_mat() refuses.  Out of line: a call checks up to a dozen matrices, and formatting
 // their names cost it most of a microsecond.
-[[gnu::cold, gnu::noinline]] int mat_error(const lq_mat& m, const char* what, int index) {
+[[gnu::cold, gnu::noinline]] static int mat_error(const lq_mat& m, const char* what, int index) {
   char name[32];
   if (index >= 0) snprintf(name, sizeof(name), "%s[%d]", what, index);
   else snprintf(name, sizeof(name), "%s", what);
@@ -95,6 +93,8 @@ int check_mat(const lq_mat& m, const char* what, int index, bool need_data) {
     good = m.ld >= m.cols && (m.data ? aligned(m.data, dtype_size(m.dtype)) : !need_data);
   return good ? LQ_OK : mat_error(m, what, index);
 }
+
+namespace {
 
 // Validates star + model (+ optional P) and works out the common dtype and the joined width.
 struct Checked {

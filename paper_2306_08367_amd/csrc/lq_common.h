@@ -48,6 +48,9 @@ int num_cus();
 // one resident set only start when earlier ones end, at whatever occupancy is then left.
 int resident_per_cu(const void* kernel, int threads, size_t lds);
 
+// LQ_OK, or the error that says what is wrong with a matrix (`index` >= 0: the message names entry `index` of the array `what`).
+int check_mat(const lq_mat& m, const char* what, int index, bool need_data);
+
 // Everything a predict kernel needs, passed by value as the kernel argument.
 struct PredictArgs {
   int64_t n;

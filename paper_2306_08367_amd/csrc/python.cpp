@@ -14,6 +14,7 @@
 #include <ATen/EmptyTensor.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -808,6 +809,242 @@ template <bool WIDE> PyObject* keymap_lookup(PyObject* const* a) {
   return a[2] != Py_None ? (Py_INCREF(a[2]), a[2]) : wrap(fk);
 }
 
+// ------------------------------------------------------------------ grouped operators ---
+
+// A tensor that must live on `dev`, the GPU of the call.
+const at::Tensor& on(PyObject* o, const at::Device& dev, const char* what) {
+  const at::Tensor& t = tensor(o);
+  if (t.device() != dev) {
+    PyErr_Format(PyExc_ValueError, "%s must live on the GPU of the call's other tensors", what);
+    throw PyErrorSet{};
+  }
+  return t;
+}
+const at::Device gpu_of(PyObject* o, const char* what) {
+  const at::Tensor& t = tensor(o);
+  if (!t.is_cuda()) {
+    PyErr_Format(PyExc_ValueError, "%s must live on the GPU", what);
+    throw PyErrorSet{};
+  }
+  return t.device();
+}
+lq_mat mat_on(PyObject* o, const at::Device& dev, const char* what) {
+  on(o, dev, what);
+  return mat(o);
+}
+
+// A [count x rows x cols] tensor as a stack of matrices.
+lq_stack stack_on(PyObject* o, const at::Device& dev, const char* what) {
+  const at::Tensor& t = on(o, dev, what);
+  if (t.dim() != 3) {
+    PyErr_Format(PyExc_ValueError, "%s must be a 3-D tensor (a matrix per group)", what);
+    throw PyErrorSet{};
+  }
+  for (int d = 0; d < 3; ++d)
+    if (t.size(d) > INT32_MAX) raise(PyExc_ValueError, "a stack of matrices has a size beyond 32 bits");
+  const int32_t g = static_cast<int32_t>(t.size(0)), r = static_cast<int32_t>(t.size(1)), c = static_cast<int32_t>(t.size(2));
+  const int32_t dt = dtype_code(o, t);
+  if (c > 1 && t.stride(2) != 1) raise(PyExc_ValueError, "matrix columns must be contiguous (row-major)");
+  const int64_t ld = r > 1 ? t.stride(1) : std::max<int64_t>(c, 1);
+  if (r > 1 && ld < c) raise(PyExc_ValueError, "row stride smaller than the row");
+  return lq_stack{t.data_ptr(), g, r, c, dt, ld, g > 1 ? t.stride(0) : 0};
+}
+
+// offsets [n_groups + 1] and order [n] (or None, then `n` says how many positions there are).
+lq_groups groups_on(PyObject* offsets, PyObject* order, int64_t n, int32_t n_groups, const at::Device& dev) {
+  on(offsets, dev, "offsets");
+  const at::Tensor& off = expect_i32(offsets, "offsets");
+  if (length(off) != static_cast<int64_t>(n_groups) + 1) raise(PyExc_ValueError, "offsets must have one entry more than there are groups");
+  lq_groups g{n, n_groups, static_cast<const int32_t*>(off.data_ptr()), nullptr};
+  if (order != Py_None) {
+    on(order, dev, "order");
+    const at::Tensor& o = expect_i32(order, "order");
+    if (length(o) != n) raise(PyExc_ValueError, "order must have one entry per position");
+    g.order = static_cast<const int32_t*>(o.data_ptr());
+  }
+  return g;
+}
+
+// The caller's workspace, or one of `bytes` bytes (of `least` at the least); nothing where none is needed.
+at::Tensor workspace(PyObject* given, size_t bytes, size_t least, const at::Device& dev, const Stream& s) {
+  if (given != Py_None) {
+    const at::Tensor& t = on(given, dev, "ws");
+    if (!t.is_contiguous()) raise(PyExc_ValueError, "ws must be contiguous");
+    return t;
+  }
+  const size_t need = std::max(bytes, least);
+  return need ? empty({static_cast<int64_t>(need)}, at::kByte, dev, s) : at::Tensor();
+}
+void* ws_data(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+size_t ws_size(const at::Tensor& t) { return t.defined() ? bytes_of(t) : 0; }
+
+PyObject* given_or(PyObject* given, const at::Tensor& made) {
+  if (given == Py_None) return wrap_or_none(made);
+  Py_INCREF(given);
+  return given;
+}
+
+uint32_t check_flag(PyObject* o) {
+  const int64_t flags = integer(o);
+  if (flags & ~static_cast<int64_t>(LQ_CHECK_FKS)) raise(PyExc_ValueError, "flags: LQ_CHECK_FKS or 0");
+  return static_cast<uint32_t>(flags);
+}
+int32_t size32(PyObject* o, const char* what) {
+  const int64_t v = integer(o);
+  if (v != static_cast<int32_t>(v)) {
+    PyErr_Format(PyExc_ValueError, "%s does not fit 32 bits", what);
+    throw PyErrorSet{};
+  }
+  return static_cast<int32_t>(v);
+}
+
+// (keys, n_groups, offsets, order, flags, ws, stream) -> (offsets, order)
+PyObject* group_rows(PyObject* const* a) {
+  const Stream s(a[6]);
+  const at::Tensor& keys = expect_i32(a[0], "keys");
+  const at::Device dev = gpu_of(a[0], "keys");
+  const c10::DeviceGuard guard(dev);
+  const int64_t n = length(keys);
+  if (keys.dim() != 1) raise(PyExc_ValueError, "keys must be a 1-D tensor");
+  const int32_t G = size32(a[1], "n_groups");
+  if (G < 1 || G > LQ_MAX_MODELS) raise(PyExc_ValueError, "n_groups outside 1..LQ_MAX_MODELS");
+  const uint32_t flags = check_flag(a[4]);
+  at::Tensor off, order;
+  if (a[2] != Py_None) {
+    on(a[2], dev, "offsets");
+    off = expect_i32(a[2], "offsets");
+    if (off.dim() != 1 || length(off) != static_cast<int64_t>(G) + 1) raise(PyExc_ValueError, "offsets must have one entry more than there are groups");
+  } else {
+    off = empty({static_cast<int64_t>(G) + 1}, at::kInt, dev, s);
+  }
+  if (a[3] != Py_None) {
+    on(a[3], dev, "order");
+    order = expect_i32(a[3], "order");
+    if (order.dim() != 1 || length(order) != n) raise(PyExc_ValueError, "order must have one entry per key");
+  } else {
+    order = empty({n}, at::kInt, dev, s);
+  }
+  const at::Tensor ws = workspace(a[5], lq_group_rows_workspace_bytes(n, G), flags ? 256 : 0, dev, s);
+  const int32_t* kp = static_cast<const int32_t*>(keys.data_ptr());
+  int32_t *op = static_cast<int32_t*>(off.data_ptr()), *rp = static_cast<int32_t*>(order.data_ptr());
+  call(s, [&](void* stream) { return lq_group_rows(kp, n, G, op, rp, ws_data(ws), ws_size(ws), flags, stream); });
+  PyObject* o = given_or(a[2], off);
+  return pair(o, given_or(a[3], order));
+}
+
+// (X, W, offsets, order, bias, gate, Y, y_dtype, transposed, relu, x_grouped, y_grouped, x_slots, flags, ws, stream)
+PyObject* grouped_product(PyObject* const* a) {
+  const Stream s(a[15]);
+  const at::Device dev = gpu_of(a[0], "X");
+  const c10::DeviceGuard guard(dev);
+  const lq_mat X = mat_on(a[0], dev, "X");
+  const lq_stack W = stack_on(a[1], dev, "W");
+  const int32_t slots = size32(a[12], "x_slots");
+  if (slots < 1) raise(PyExc_ValueError, "x_slots must be at least 1");
+  const int64_t n = a[3] != Py_None ? length(tensor(a[3])) : X.rows * slots;
+  const lq_groups groups = groups_on(a[2], a[3], n, W.count, dev);
+  uint32_t flags = check_flag(a[13]);
+  const bool checked = flags != 0, transposed = truth(a[8]);
+  flags |= (transposed ? LQ_TRANSPOSED : 0) | (truth(a[9]) ? LQ_RELU : 0) | (truth(a[10]) ? LQ_X_GROUPED : 0) | (truth(a[11]) ? LQ_Y_GROUPED : 0);
+  lq_mat bias{}, gate{};
+  if (a[4] != Py_None) bias = mat_on(a[4], dev, "bias");
+  if (a[5] != Py_None) gate = mat_on(a[5], dev, "gate");
+  const int32_t l = transposed ? W.rows : W.cols;
+  const at::Tensor Y = a[6] != Py_None ? on(a[6], dev, "Y") : empty({n, l}, scalar_type(a[7], tensor(a[0]).scalar_type()), dev, s);
+  const at::Tensor ws = workspace(a[14], lq_grouped_workspace_bytes(n, W.count, W.rows, W.cols, W.dtype), checked ? 256 : 0, dev, s);
+  PyObject* out = given_or(a[6], Y);
+  try {
+    lq_mat Ym = mat(out);
+    call(s, [&](void* stream) {
+      return lq_grouped_product(&groups, &X, slots, &W, a[4] != Py_None ? &bias : nullptr, a[5] != Py_None ? &gate : nullptr, &Ym,
+                                ws_data(ws), ws_size(ws), flags, stream);
+    });
+  } catch (...) {
+    Py_DECREF(out);
+    throw;
+  }
+  return out;
+}
+
+// (X, dY, offsets, order, dW, db, dw_dtype, want_bias, x_grouped, y_grouped, x_slots, flags, ws, stream) -> (dW, db)
+PyObject* grouped_gradient(PyObject* const* a) {
+  const Stream s(a[13]);
+  const at::Device dev = gpu_of(a[0], "X");
+  const c10::DeviceGuard guard(dev);
+  const lq_mat X = mat_on(a[0], dev, "X"), dY = mat_on(a[1], dev, "dY");
+  const int32_t slots = size32(a[10], "x_slots");
+  if (slots < 1) raise(PyExc_ValueError, "x_slots must be at least 1");
+  on(a[2], dev, "offsets");
+  const int64_t G = length(tensor(a[2])) - 1;
+  if (G < 1 || G > LQ_MAX_MODELS) raise(PyExc_ValueError, "offsets must have 2..LQ_MAX_MODELS + 1 entries");
+  const lq_groups groups = groups_on(a[2], a[3], a[3] != Py_None ? length(tensor(a[3])) : dY.rows, static_cast<int32_t>(G), dev);
+  const uint32_t check = check_flag(a[11]);
+  const uint32_t flags = check | (truth(a[8]) ? LQ_X_GROUPED : 0) | (truth(a[9]) ? LQ_Y_GROUPED : 0);
+  const at::ScalarType st = a[4] != Py_None ? tensor(a[4]).scalar_type() : scalar_type(a[6], tensor(a[0]).scalar_type());
+  const at::Tensor dW = a[4] != Py_None ? on(a[4], dev, "dW") : empty({G, X.cols, dY.cols}, st, dev, s);
+  at::Tensor db;
+  if (a[5] != Py_None) db = on(a[5], dev, "db");
+  else if (truth(a[7])) db = empty({G, dY.cols}, st, dev, s);
+  const at::Tensor ws = workspace(a[12], lq_grouped_gradient_workspace_bytes(groups.n, groups.n_groups, X.cols, dY.cols, X.dtype),
+                                  check ? 256 : 0, dev, s);
+  PyObject* w = given_or(a[4], dW);
+  PyObject* b = nullptr;
+  try {
+    b = given_or(a[5], db);
+    lq_stack dWm = stack_on(w, dev, "dW");
+    lq_mat dbm{};
+    if (b != Py_None) dbm = mat(b);
+    const bool bias = b != Py_None;
+    call(s, [&](void* stream) {
+      return lq_grouped_gradient(&groups, &X, slots, &dY, &dWm, bias ? &dbm : nullptr, ws_data(ws), ws_size(ws), flags, stream);
+    });
+  } catch (...) {
+    Py_DECREF(w);
+    Py_XDECREF(b);
+    throw;
+  }
+  return pair(w, b);
+}
+
+// (X, W, A, B, offsets, order, scale, bias, Y, y_dtype, flags, ws, stream)
+PyObject* adapter_product(PyObject* const* a) {
+  const Stream s(a[12]);
+  const at::Device dev = gpu_of(a[0], "X");
+  const c10::DeviceGuard guard(dev);
+  const lq_mat X = mat_on(a[0], dev, "X"), W = mat_on(a[1], dev, "W");
+  const lq_stack A = stack_on(a[2], dev, "A"), B = stack_on(a[3], dev, "B");
+  const lq_groups groups = groups_on(a[4], a[5], X.rows, A.count, dev);
+  const float* scale = nullptr;
+  if (a[6] != Py_None) {
+    on(a[6], dev, "scale");
+    const at::Tensor& t = expect(a[6], at::kFloat, "torch.float32", "scale");
+    if (t.dim() != 1 || t.size(0) != A.count) raise(PyExc_ValueError, "scale must have one entry per adapter");
+    scale = static_cast<const float*>(t.data_ptr());
+  }
+  lq_mat bias{};
+  if (a[7] != Py_None) {
+    const at::Tensor& t = on(a[7], dev, "bias");
+    if (t.dim() != 1 || t.size(0) != W.cols || (t.size(0) > 1 && t.stride(0) != 1))
+      raise(PyExc_ValueError, "bias must be a contiguous 1-D tensor with an entry per column of W");
+    bias = lq_mat{t.data_ptr(), 1, W.cols, std::max(W.cols, 1), dtype_code(a[7], t)};
+  }
+  const uint32_t flags = check_flag(a[10]);
+  const at::Tensor Y = a[8] != Py_None ? on(a[8], dev, "Y") : empty({X.rows, W.cols}, scalar_type(a[9], tensor(a[0]).scalar_type()), dev, s);
+  const at::Tensor ws = workspace(a[11], lq_adapter_workspace_bytes(X.rows, A.count, static_cast<int32_t>(W.rows), W.cols, A.cols, X.dtype), 256, dev, s);
+  PyObject* out = given_or(a[8], Y);
+  try {
+    lq_mat Ym = mat(out);
+    call(s, [&](void* stream) {
+      return lq_adapter_product(&groups, &X, &W, a[7] != Py_None ? &bias : nullptr, &A, &B, scale, &Ym, ws_data(ws), ws_size(ws), flags,
+                                stream);
+    });
+  } catch (...) {
+    Py_DECREF(out);
+    throw;
+  }
+  return out;
+}
+
 // ------------------------------------------------------------------ module --------------
 
 // The module's functions take a fixed number of positional arguments; C++ exceptions end here.
@@ -861,6 +1098,10 @@ PyMethodDef methods[] = {
     LQ_PY("fused_join_tree_masks", fused_join_tree_masks, 11),
     LQ_PY("keymap_build", keymap_build<false>, 4),
     LQ_PY("keymap64_build", keymap_build<true>, 4),
+    LQ_PY("group_rows", group_rows, 7),
+    LQ_PY("grouped_product", grouped_product, 16),
+    LQ_PY("grouped_gradient", grouped_gradient, 14),
+    LQ_PY("adapter_product", adapter_product, 13),
     LQ_PY("keymap_lookup", keymap_lookup<false>, 4),
     LQ_PY("keymap64_lookup", keymap_lookup<true>, 4),
     {nullptr, nullptr, 0, nullptr}};
