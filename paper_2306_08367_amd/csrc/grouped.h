@@ -84,12 +84,29 @@ template <typename T> __device__ __forceinline__ u32x4 load_piece(const T* p, in
   return r;
 }
 
-// Position range and group of row tile t of TM rows: the tiles of group 0, of group 1, ..., then those of the rows
-// without a group (group -1).  rows == 0: there is no such tile.  Called by a whole wavefront: lane l adds up the
-// tiles of groups l * per .. l * per + per - 1, the sums are scanned over the lanes, and the lane that holds t walks
-// its groups again.
-struct RowTile { int group, first, rows; };
-template <int TM> __device__ __forceinline__ RowTile find_row_tile(const int32_t* __restrict__ off, int G, int n, int t) {
+// Workgroups go to the 8 dies in turn; each die gets a contiguous run of tiles, so that neighbouring tiles, which
+// share rows or a matrix, share an L2.
+__device__ __forceinline__ int die_order(int id, int total) {
+  const int per = total >> 3, more = total & 7, die = id & 7, at = id >> 3;
+  return die * per + min(die, more) + at;
+}
+
+// The tile that workgroup `id` works on: TM rows of one group and one of `cols` column tiles.  Tiles are numbered group by
+// group, then those of the rows without a group (group -1); inside a group by runs of 8 row tiles, the rows of a run
+// fastest, so that neighbouring tiles share the rows of X and the columns of the matrix about evenly.  rows == 0: there is
+// no such tile.  Called by a whole wavefront: lane l adds up the row tiles of groups l * per .. l * per + per - 1, the sums are
+// scanned over the lanes, and the lane that holds the tile walks its groups again.
+struct RowTile { int group, first, rows, col; };
+// Tile `local` of positions [begin, end).
+template <int TM> __device__ __forceinline__ RowTile tile_of_range(int group, int begin, int end, int local, int cols) {
+  constexpr int RUN = 8;
+  const int run = local / (RUN * cols), tiles = (end - begin + TM - 1) / TM;
+  const int in_run = min(RUN, tiles - run * RUN), left = local - run * RUN * cols;
+  if (in_run <= 0) return {group, begin, 0, 0};
+  const int first = begin + (run * RUN + left % in_run) * TM;
+  return {group, first, min(TM, end - first), left / in_run};
+}
+template <int TM> __device__ __forceinline__ RowTile find_tile(const int32_t* __restrict__ off, int G, int n, int id, int cols) {
   const int lane = threadIdx.x & 63;
   const int per = (G + 63) >> 6;
   const int g0 = min(lane * per, G), g1 = min(g0 + per, G);
@@ -101,54 +118,58 @@ template <int TM> __device__ __forceinline__ RowTile find_row_tile(const int32_t
     const int v = __shfl_up(upto, d);
     if (lane >= d) upto += v;
   }
-  const int total = __shfl(upto, 63);
-  if (t >= total) {
-    const int first = off[G] + (t - total) * TM;
-    return {-1, first, max(0, min(TM, n - first))};
-  }
-  const unsigned long long holds = __ballot(upto > t);
-  const int at = __ffsll(static_cast<long long>(holds)) - 1;
-  int left = t - (upto - own), group = 0, first = 0, rows = 0;
-  if (lane == at) {
-    for (int g = g0; g < g1; ++g) {
-      const int b = off[g], e = off[g + 1], tiles = (e - b + TM - 1) / TM;
-      if (left < tiles) {
-        group = g;
-        first = b + left * TM;
-        rows = min(TM, e - first);
-        break;
+  const int total = __builtin_amdgcn_readlane(upto, 63);
+  int group = -1, begin = __builtin_amdgcn_readfirstlane(off[G]), end = n, before = total;   // of the group: its positions, row tiles before it
+  const int tiles = (total + (n - begin + TM - 1) / TM) * cols;
+  if (id >= tiles) return {-1, 0, 0, 0};
+  id = die_order(id, tiles);
+  const int t = id / cols;
+  if (t < total) {
+    const unsigned long long holds = __ballot(upto > t);
+    const int at = __ffsll(static_cast<long long>(holds)) - 1;
+    if (lane == at) {
+      before = upto - own;
+      for (int g = g0; g < g1; ++g) {
+        const int b = off[g], e = off[g + 1], more = (e - b + TM - 1) / TM;
+        if (t < before + more) {
+          group = g;
+          begin = b;
+          end = e;
+          break;
+        }
+        before += more;
       }
-      left -= tiles;
     }
+    group = __builtin_amdgcn_readlane(group, at);
+    begin = __builtin_amdgcn_readlane(begin, at);
+    end = __builtin_amdgcn_readlane(end, at);
+    before = __builtin_amdgcn_readlane(before, at);
   }
-  return {__shfl(group, at), __shfl(first, at), __shfl(rows, at)};
+  return tile_of_range<TM>(group, begin, end, id - before * cols, cols);
 }
-
-// Workgroups go to the 8 dies in turn; each die gets a contiguous run of tiles, so that neighbouring tiles, which
-// share rows or a matrix, share an L2.
-__device__ __forceinline__ int die_order(int id, int total) {
-  const int per = total >> 3, more = total & 7, die = id & 7, at = id >> 3;
-  return die * per + min(die, more) + at;
+// The same where all positions use one matrix (group 0).
+template <int TM> __device__ __forceinline__ RowTile all_rows(int n, int id, int cols) {
+  return tile_of_range<TM>(0, 0, n, die_order(id, (n + TM - 1) / TM * cols), cols);
 }
 
 // One operand of the tile product in LDS: EXT rows of the result (or columns) by KSTEP of the inner dimension, as
 // lines of 16-byte pieces.
-//   KMAJ    a line per row, the inner dimension along it (128 bytes): a lane's operand is one 16-byte read
+//   KMAJ    a line per row, the inner dimension along it (KBYTES bytes): a lane's operand is one 16-byte read
 //   !KMAJ   a line per inner index, the rows along it: bf16 operands come transposed out of LDS
 //           (ds_read_b64_tr_b16: four inner indexes of a row a lane), fp32 ones a word at a time
 // Piece c of a line lies at place c ^ spread(line), so that the lanes of a read use all banks.
-template <typename T, bool KMAJ, int EXT, int THREADS> struct Operand {
+template <typename T, bool KMAJ, int EXT, int THREADS, int KBYTES = 128> struct Operand {
   static constexpr int EPC = 16 / sizeof(T);
-  static constexpr int KSTEP = 128 / sizeof(T);
+  static constexpr int KSTEP = KBYTES / sizeof(T);
   static constexpr int LINES = KMAJ ? EXT : KSTEP;
-  static constexpr int CPL = KMAJ ? 8 : EXT / EPC;
+  static constexpr int CPL = KMAJ ? KBYTES / 16 : EXT / EPC;
   static constexpr int PIECES = LINES * CPL;
   static constexpr int PER = PIECES / THREADS;
   static constexpr int BYTES = PIECES * 16;
   static_assert(PIECES % THREADS == 0, "whole pieces a thread");
 
   static __device__ __forceinline__ int spread(int line) {
-    if constexpr (KMAJ) return (line >> 1) & 7;
+    if constexpr (KMAJ) return CPL == 8 ? (line >> 1) & 7 : (line >> 2) & 3;
     else if constexpr (sizeof(T) == 4) return 4 * ((line >> 2) & 3);
     else if constexpr (CPL >= 16) return 2 * ((line & 3) | ((line >> 1) & 4));
     else return 2 * (((line >> 1) & 1) | ((line >> 2) & 2));
@@ -225,9 +246,88 @@ __device__ __forceinline__ void multiply_step(const char* la, const char* lb, f3
   }
 }
 
-// 16 bytes from memory straight into LDS: lane l's land at base + 16 l (`base` is the wavefront's).
-__device__ __forceinline__ void copy_to_lds(const void* p, char* base) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)base, 16, 0, 0);
+// 16 bytes a lane from memory straight into LDS: lane l's land at base + 16 l (`base`: LDS byte address, the same in all
+// lanes).  Written as an instruction because the compiler, which sees LDS written by its own form of it, waits for all
+// copies before the next transposed read of LDS, also where that reads another buffer.  It has no result in registers;
+// the compiler does not count it: meet_after_copies() waits for it.  It writes m0, which nothing else in these kernels
+// uses (the compiler takes no m0 in a list of what an instruction overwrites; a test reads the assembly for it).
+__device__ __forceinline__ void copy_to_lds(const void* p, unsigned int base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(base)), "v"(p));
+}
+__device__ __forceinline__ unsigned int lds_address(const char* p) {
+  return static_cast<unsigned int>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)p));
+}
+// All copies of this wavefront and its reads and writes of LDS are done; then the workgroup meets.
+__device__ __forceinline__ void meet_after_copies() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// A point that no instruction is moved over.
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+
+// The product of a tile of 8 wavefronts, two on a SIMD, over `units` blocks of 32 inner indexes: issue(u, LDS address) copies
+// block u's operands to LDS, in COPIES instructions a wavefront.  The two wavefronts of a SIMD take turns: while one
+// multiplies a block (32 matrix instructions, 512 clocks), the other one reads its operands of its next block from LDS, so
+// that neither the matrix cores nor LDS wait for the other.  The second four wavefronts run one turn behind the
+// first four, by one barrier more at the start.  In turns: the first four read block u in turn 2 u and multiply it
+// in turn 2 u + 1, the second four one later.  LDS holds four blocks.  Block u + 3 takes the place of block u - 1, whose
+// last readers are the second four in turn 2 u - 1: each wavefront issues its copies for it when it begins to read block u,
+// and waits for its copies of block u + 1 at the end of turn 2 u + 1, with those of two blocks still in flight: they have
+// five or six turns to arrive.
+template <typename T, class S, class A, class B, typename F>
+__device__ __forceinline__ void multiply_in_turns(char* lds, int units, F&& issue, f32x4 (&acc)[S::MI][S::NI]) {
+  static_assert(S::THREADS == 512 && S::WAVES_N == 4, "two wavefronts a SIMD");
+  constexpr int BLOCK = A::BYTES + B::BYTES, COPIES = A::PER + B::PER;
+  static_assert(COPIES == 4, "the waits below count copies");
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool second = wave >= 4;
+  const int m0 = (wave / S::WAVES_N) * S::MI * 16, n0 = (wave % S::WAVES_N) * S::NI * 16;
+  const unsigned int at = lds_address(lds);
+  auto turn = [&]() {
+    fence();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    fence();
+  };
+  // (the copies of the two youngest blocks may be in flight; at the end there are no younger ones)
+  auto wait_copies = [&](bool younger) {
+    fence();
+    if (younger) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  };
+  for (int u = 0; u < min(units, 3); ++u) issue(u, at + u * BLOCK);
+  wait_copies(units >= 3);
+  turn();
+  if (second) turn();
+  for (int u = 0; u < units; ++u) {
+    const char* from = lds + (u & 3) * BLOCK;
+    if (u + 3 < units) issue(u + 3, at + ((u + 3) & 3) * BLOCK);
+    u32x4 a[S::MI], b[S::NI];
+#pragma unroll
+    for (int j = 0; j < S::NI; ++j) b[j] = B::fragment(from + A::BYTES, n0 + 16 * j, 0);
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) a[i] = A::fragment(from, m0 + 16 * i, 0);
+    if (second) wait_copies(u + 3 < units);
+    turn();
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NI; ++j) acc[i][j] = multiply<T>(b[j], a[i], acc[i][j]);
+    __builtin_amdgcn_s_setprio(0);
+    if (!second) wait_copies(u + 3 < units);
+    turn();
+  }
+  if (!second) turn();
+}
+
+// Four by four exchange of registers and groups of 16 lanes: register j of lanes 16 g .. 16 g + 15 and register g of lanes 16 j .. .
+// A row's results, four neighbouring columns a lane and 16-column block, become 16 neighbouring columns a lane.
+__device__ __forceinline__ void exchange(unsigned int& r0, unsigned int& r1, unsigned int& r2, unsigned int& r3) {
+  typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+  u32x2 p = __builtin_amdgcn_permlane32_swap(r0, r2, false, false), q = __builtin_amdgcn_permlane32_swap(r1, r3, false, false);
+  u32x2 s = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false), t = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
+  r0 = s[0];
+  r1 = s[1];
+  r2 = t[0];
+  r3 = t[1];
 }
 
 #endif  // __HIPCC__

@@ -14,7 +14,7 @@ __global__ __launch_bounds__(S::THREADS) void grouped_gradient_kernel(GradientAr
   typedef Operand<T, false, S::TN, S::THREADS> B;
   constexpr int KSTEP = A::KSTEP, EPC = A::EPC, THREADS = S::THREADS;
   extern __shared__ __align__(1024) char lds[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int id = die_order(blockIdx.x, gridDim.x);
   const int per_group = a.tiles_m * a.tiles_n;
   const int group = id / per_group, tm = id % per_group / a.tiles_n, tn = id % a.tiles_n;
@@ -49,18 +49,19 @@ __global__ __launch_bounds__(S::THREADS) void grouped_gradient_kernel(GradientAr
   };
   u32x4 ra[DIRECT ? 1 : A::PER], rb[DIRECT ? 1 : B::PER];
   auto fetch = [&](char* to) {
+    const unsigned int at = DIRECT ? lds_address(to) : 0;
 #pragma unroll
     for (int i = 0; i < A::PER; ++i) {
       const int c = m0 + A::piece_of(i) * EPC;
       const T* p = X + xr[i] * a.ldx + c;
-      if constexpr (DIRECT) copy_to_lds(xr[i] >= 0 && c < a.k ? static_cast<const void*>(p) : &g_zeros, to + (i * THREADS + wave * 64) * 16);
+      if constexpr (DIRECT) copy_to_lds(xr[i] >= 0 && c < a.k ? static_cast<const void*>(p) : &g_zeros, at + (i * THREADS + wave * 64) * 16);
       else ra[i] = load_piece(p, xr[i] >= 0 ? a.k - c : 0);
     }
 #pragma unroll
     for (int i = 0; i < B::PER; ++i) {
       const int c = n0 + B::piece_of(i) * EPC;
       const T* p = dY + yr[i] * a.ldy + c;
-      if constexpr (DIRECT) copy_to_lds(yr[i] >= 0 && c < a.l ? static_cast<const void*>(p) : &g_zeros, to + A::BYTES + (i * THREADS + wave * 64) * 16);
+      if constexpr (DIRECT) copy_to_lds(yr[i] >= 0 && c < a.l ? static_cast<const void*>(p) : &g_zeros, at + A::BYTES + (i * THREADS + wave * 64) * 16);
       else rb[i] = load_piece(p, yr[i] >= 0 ? a.l - c : 0);
     }
   };
@@ -80,7 +81,8 @@ __global__ __launch_bounds__(S::THREADS) void grouped_gradient_kernel(GradientAr
     look_up(KSTEP);
     int at = 0;
     for (int k0 = 0; k0 < rows; k0 += KSTEP, at ^= 1) {
-      __syncthreads();     // this buffer is whole, the other one is read to its end
+      if constexpr (DIRECT) meet_after_copies();
+      else __syncthreads();     // this buffer is whole, the other one is read to its end
       const bool more = k0 + KSTEP < rows;
       if (more) {
         fetch(lds + (at ^ 1) * BUFFER);

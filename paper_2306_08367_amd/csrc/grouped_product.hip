@@ -50,25 +50,25 @@ __device__ __forceinline__ void store_four(void* row, int n, int valid, f32x4 v,
 
 template <typename T, class S, bool BT, bool DIRECT, bool ADAPT>
 __global__ __launch_bounds__(S::THREADS) void grouped_product_kernel(GroupedArgs a) {
-  typedef Operand<T, true, S::TM, S::THREADS> A;
-  typedef Operand<T, BT, S::TN, S::THREADS> B;
+  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
+  typedef Operand<T, true, S::TM, S::THREADS, KBYTES> A;
+  typedef Operand<T, BT, S::TN, S::THREADS, KBYTES> B;
   constexpr int KSTEP = A::KSTEP, EPC = A::EPC, THREADS = S::THREADS;
   extern __shared__ __align__(1024) char lds[];
   __shared__ int xrow[S::TM], yrow[S::TM];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  const int id = die_order(blockIdx.x, gridDim.x);
-  const int n0 = (id % a.tiles_n) * S::TN, t = id / a.tiles_n;
   RowTile tile;
-  if constexpr (ADAPT) tile = {0, t * S::TM, min(S::TM, a.n - t * S::TM)};
-  else tile = find_row_tile<S::TM>(a.off, a.G, a.n, t);
+  if constexpr (ADAPT) tile = all_rows<S::TM>(a.n, blockIdx.x, a.tiles_n);
+  else tile = find_tile<S::TM>(a.off, a.G, a.n, blockIdx.x, a.tiles_n);
+  const int n0 = tile.col * S::TN;
   if (tile.rows <= 0) return;
 
   for (int m = tid; m < S::TM; m += THREADS) {
-    const int p = tile.first + m;
     const bool in = m < tile.rows;
-    const int r = in ? (a.order ? a.order[p] : p) : 0;
-    xrow[m] = in ? (a.x_grouped ? p : r / a.slots) : -1;
+    const int p = tile.first + (in ? m : tile.rows - 1);     // (behind the last row: that row again, not stored)
+    const int r = a.order ? a.order[p] : p;
+    xrow[m] = a.x_grouped ? p : r / a.slots;
     yrow[m] = a.y_grouped ? p : r;
     if (!ADAPT && a.gpos && in && n0 == 0 && blockIdx.y == 0) a.gpos[p] = tile.group;
   }
@@ -85,63 +85,80 @@ __global__ __launch_bounds__(S::THREADS) void grouped_product_kernel(GroupedArgs
   if (tile.group >= 0 && k_first < k_end) {
     const T* X = static_cast<const T*>(a.X);
     const T* W = static_cast<const T*>(a.W) + tile.group * a.sw;
-    // Where this thread's pieces of either operand lie at inner index 0 (NULL: outside), and their first inner index.
+    // Where this thread's pieces of either operand lie at inner index 0, and their first inner index.  Columns behind the
+    // last one repeat the last piece (direct copies) or are zeros; they are not stored.
     const T *pa[A::PER], *pb[B::PER];
     int va[A::PER], vb[B::PER];
 #pragma unroll
     for (int i = 0; i < A::PER; ++i) {
-      const int row = xrow[A::line_of(i)];
       va[i] = A::piece_of(i) * EPC;
-      pa[i] = row >= 0 ? X + row * a.ldx + va[i] : nullptr;
+      pa[i] = X + xrow[A::line_of(i)] * a.ldx + va[i];
     }
 #pragma unroll
     for (int i = 0; i < B::PER; ++i) {
       const int line = B::line_of(i), e = B::piece_of(i) * EPC;
-      if constexpr (BT) {
-        vb[i] = e;
-        pb[i] = n0 + line < a.N ? W + static_cast<int64_t>(n0 + line) * a.ldw + e : nullptr;
-      } else {
-        vb[i] = line;
-        pb[i] = n0 + e < a.N ? W + line * a.ldw + n0 + e : nullptr;
-      }
+      vb[i] = BT ? e : line;
+      pb[i] = BT ? W + static_cast<int64_t>(min(n0 + line, a.N - 1)) * a.ldw + e : W + line * a.ldw + (DIRECT ? min(n0 + e, a.N - EPC) : n0 + e);
     }
     const int64_t step_b = BT ? 1 : a.ldw;     // elements per inner index
     constexpr int BUFFER = A::BYTES + B::BYTES;
 
-    u32x4 ra[DIRECT ? 1 : A::PER], rb[DIRECT ? 1 : B::PER];
-    auto fetch = [&](int k0, char* to) {
-      if constexpr (DIRECT) {
+    if constexpr (DIRECT) {
+      auto issue = [&](int step, unsigned int to) {
+        const int k0 = k_first + step * KSTEP;
+        to += wave * 1024;
+        if (k0 + KSTEP <= k_end) {
 #pragma unroll
-        for (int i = 0; i < A::PER; ++i)
-          copy_to_lds(pa[i] && k0 + va[i] < k_end ? static_cast<const void*>(pa[i] + k0) : &g_zeros, to + (i * THREADS + wave * 64) * 16);
+          for (int i = 0; i < A::PER; ++i) copy_to_lds(pa[i] + k0, to + i * THREADS * 16);
 #pragma unroll
-        for (int i = 0; i < B::PER; ++i)
-          copy_to_lds(pb[i] && k0 + vb[i] < k_end ? static_cast<const void*>(pb[i] + k0 * step_b) : &g_zeros,
-                      to + A::BYTES + (i * THREADS + wave * 64) * 16);
+          for (int i = 0; i < B::PER; ++i) copy_to_lds(pb[i] + k0 * step_b, to + A::BYTES + i * THREADS * 16);
+        } else {
+#pragma unroll
+          for (int i = 0; i < A::PER; ++i)
+            copy_to_lds(k0 + va[i] < k_end ? static_cast<const void*>(pa[i] + k0) : &g_zeros, to + i * THREADS * 16);
+#pragma unroll
+          for (int i = 0; i < B::PER; ++i)
+            copy_to_lds(k0 + vb[i] < k_end ? static_cast<const void*>(pb[i] + k0 * step_b) : &g_zeros, to + A::BYTES + i * THREADS * 16);
+        }
+      };
+      const int steps = (k_end - k_first + KSTEP - 1) / KSTEP;
+      if constexpr (THREADS == 512) {
+        multiply_in_turns<T, S, A, B>(lds, steps, issue, acc);
       } else {
+        issue(0, lds_address(lds));
+        for (int step = 0; step < steps; ++step) {
+          const int at = (step & 1) * BUFFER;
+          meet_after_copies();     // this buffer is whole, the other one is read to its end
+          if (step + 1 < steps) issue(step + 1, lds_address(lds) + (at ^ BUFFER));
+          multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc);
+        }
+      }
+      __syncthreads();
+    } else {
+      u32x4 ra[A::PER], rb[B::PER];
+      auto fetch = [&](int k0) {
 #pragma unroll
-        for (int i = 0; i < A::PER; ++i) ra[i] = load_piece(pa[i] + k0, pa[i] ? k_end - (k0 + va[i]) : 0);
+        for (int i = 0; i < A::PER; ++i) ra[i] = load_piece(pa[i] + k0, k_end - (k0 + va[i]));
 #pragma unroll
         for (int i = 0; i < B::PER; ++i)
-          rb[i] = load_piece(pb[i] + k0 * step_b, !pb[i] ? 0 : BT ? k_end - (k0 + vb[i]) : k0 + vb[i] < k_end ? a.N - n0 - B::piece_of(i) * EPC : 0);
-      }
-    };
-    auto put = [&](char* to) {
-      if constexpr (!DIRECT) {
+          rb[i] = load_piece(pb[i] + k0 * step_b, BT ? k_end - (k0 + vb[i]) : k0 + vb[i] < k_end ? a.N - n0 - B::piece_of(i) * EPC : 0);
+      };
+      auto put = [&](char* to) {
 #pragma unroll
         for (int i = 0; i < A::PER; ++i) *reinterpret_cast<u32x4*>(to + (i * THREADS + tid) * 16) = ra[i];
 #pragma unroll
         for (int i = 0; i < B::PER; ++i) *reinterpret_cast<u32x4*>(to + A::BYTES + (i * THREADS + tid) * 16) = rb[i];
+      };
+      fetch(k_first);
+      put(lds);
+      int at = 0;
+      for (int k0 = k_first; k0 < k_end; k0 += KSTEP, at ^= BUFFER) {
+        __syncthreads();     // this buffer is whole, the other one is read to its end
+        if (k0 + KSTEP < k_end) fetch(k0 + KSTEP);
+        multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc);
+        if (k0 + KSTEP < k_end) put(lds + (at ^ BUFFER));
       }
-    };
-    fetch(k_first, lds);
-    put(lds);
-    int at = 0;
-    for (int k0 = k_first; k0 < k_end; k0 += KSTEP, at ^= 1) {
-      __syncthreads();     // this buffer is whole, the other one is read to its end
-      if (k0 + KSTEP < k_end) fetch(k0 + KSTEP, lds + (at ^ 1) * BUFFER);
-      multiply_step<T, S, A, B>(lds + at * BUFFER, lds + at * BUFFER + A::BYTES, acc);
-      if (k0 + KSTEP < k_end) put(lds + (at ^ 1) * BUFFER);
+      __syncthreads();
     }
   }
 
@@ -257,12 +274,60 @@ __global__ __launch_bounds__(S::THREADS) void grouped_product_kernel(GroupedArgs
     }
   }
 
-  const int wm = (wave / S::WAVES_N) * S::MI * 16, wn = (wave % S::WAVES_N) * S::NI * 16;
+  const int wm = (wave / S::WAVES_N) * S::MI * 16, wn = n0 + (wave % S::WAVES_N) * S::NI * 16;
   const bool has_bias = a.bias && tile.group >= 0;
   const T* bias = static_cast<const T*>(a.bias) + (has_bias ? tile.group * a.ldb : 0);
+  char* const Y = static_cast<char*>(a.Y) + blockIdx.y * a.split_stride * (a.y_bf16 ? 2 : 4);
+  if (S::NI == 4 && a.y_vec && wn + 64 <= a.n_store && wn + 64 <= a.N) {
+    // 16 neighbouring columns of a row a lane
+    const int n = wn + 16 * (lane >> 4);
+    f32x4 bv[4] = {};
+    if (has_bias)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) bv[q] = load_four(bias + n + 4 * q, 4, true);
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) {
+      unsigned int v[4][4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j][q] = __float_as_uint(acc[i][j < S::NI ? j : 0][q]);
+        exchange(v[0][q], v[1][q], v[2][q], v[3][q]);
+      }
+      const int m = wm + 16 * i + (lane & 15);
+      if (m >= tile.rows) continue;
+      const int64_t r = yrow[m];
+      f32x4 y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float x = __uint_as_float(v[j][q]) + bv[j][q];
+          y[j][q] = a.relu && x < 0.f ? 0.f : x;
+        }
+        if (a.gate) {
+          const f32x4 h = load_four(static_cast<const T*>(a.gate) + r * a.ldg + n + 4 * j, 4, true);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) y[j][q] = h[q] > 0.f ? y[j][q] : 0.f;
+        }
+      }
+      if (a.y_bf16) {
+        uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<bf16_t*>(Y) + r * a.ldy + n);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          to[h] = uint4{f32x2_to_bf16x2(y[2 * h][0], y[2 * h][1]), f32x2_to_bf16x2(y[2 * h][2], y[2 * h][3]),
+                        f32x2_to_bf16x2(y[2 * h + 1][0], y[2 * h + 1][1]), f32x2_to_bf16x2(y[2 * h + 1][2], y[2 * h + 1][3])};
+      } else {
+        f32x4* to = reinterpret_cast<f32x4*>(reinterpret_cast<float*>(Y) + r * a.ldy + n);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) to[h] = y[h];
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < S::NI; ++j) {
-    const int n = n0 + wn + 16 * j + 4 * (lane >> 4), valid = a.n_store - n;
+    const int n = wn + 16 * j + 4 * (lane >> 4), valid = a.n_store - n;
     if (valid <= 0) continue;
     const bool vec = a.y_vec && valid >= 4;
     f32x4 bv = {0.f, 0.f, 0.f, 0.f};
@@ -271,7 +336,7 @@ __global__ __launch_bounds__(S::THREADS) void grouped_product_kernel(GroupedArgs
     for (int i = 0; i < S::MI; ++i) {
       const int m = wm + 16 * i + (lane & 15);
       if (m >= tile.rows) continue;
-      const int r = yrow[m];
+      const int64_t r = yrow[m];
       f32x4 v = acc[i][j] + bv;
       if (a.relu)
 #pragma unroll
@@ -281,16 +346,16 @@ __global__ __launch_bounds__(S::THREADS) void grouped_product_kernel(GroupedArgs
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = h[q] > 0.f ? v[q] : 0.f;
       }
-      char* row = static_cast<char*>(a.Y) + (blockIdx.y * a.split_stride + r * a.ldy) * (a.y_bf16 ? 2 : 4);
-      store_four(row, n, valid, v, a.y_bf16, vec);
+      store_four(Y + r * a.ldy * (a.y_bf16 ? 2 : 4), n, valid, v, a.y_bf16, vec);
     }
   }
 }
 
 template <typename T, class S, bool BT, bool DIRECT, bool ADAPT> int launch(GroupedArgs a, int splits, hipStream_t s) {
-  typedef Operand<T, true, S::TM, S::THREADS> A;
-  typedef Operand<T, BT, S::TN, S::THREADS> B;
-  constexpr int LDS = 2 * (A::BYTES + B::BYTES);
+  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
+  typedef Operand<T, true, S::TM, S::THREADS, KBYTES> A;
+  typedef Operand<T, BT, S::TN, S::THREADS, KBYTES> B;
+  constexpr int LDS = (S::THREADS == 512 ? 4 : 2) * (A::BYTES + B::BYTES);
   a.tiles_n = (a.n_store + S::TN - 1) / S::TN;
   a.row_tiles = ADAPT ? (a.n + S::TM - 1) / S::TM : a.n / S::TM + std::min(a.n, a.G + 1);
   const int steps = (a.K + A::KSTEP - 1) / A::KSTEP;
@@ -307,9 +372,12 @@ template <typename T, class S, bool BT, bool DIRECT, bool ADAPT> int launch(Grou
 
 typedef TileShape<128, 128, 2, 2> Tile128;
 typedef TileShape<64, 64, 2, 2> Tile64;
+typedef TileShape<256, 256, 2, 4> Tile256;
 
 template <typename T, bool BT, bool DIRECT, bool ADAPT> int by_size(const GroupedArgs& a, int splits, hipStream_t s) {
   const int64_t large = static_cast<int64_t>((a.n_store + 127) / 128) * ((a.n + 127) / 128);
+  if constexpr (sizeof(T) == 2 && DIRECT)
+    if (large >= 4 * num_cus()) return launch<T, Tile256, BT, DIRECT, ADAPT>(a, splits, s);
   if (large >= num_cus()) return launch<T, Tile128, BT, DIRECT, ADAPT>(a, splits, s);
   return launch<T, Tile64, BT, DIRECT, ADAPT>(a, splits, s);
 }
