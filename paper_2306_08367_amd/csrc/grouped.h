@@ -27,10 +27,9 @@ struct GroupedArgs {
   int32_t steps_per_split;   // K steps of one split; split z writes at Y + z * split_stride
   int64_t split_stride;
   int32_t* gpos;          // out: group of every position, -1 for none (or NULL)
-  // adapters: U [splits x n x rp] fp32 by position, B_g [rank x N]
-  const float* U; int64_t u_stride; int32_t u_splits, rp, rank;
+  // adapters: U [n x rp] by position, fp32 or as two bf16 numbers (the second `u_rest` elements behind the first), B_g [rank x N]
+  const void* U; int64_t u_rest; int32_t rp, rank;
   const void* B; int64_t ldB, sB;
-  const float* scale;
   const int32_t* group_of;   // gpos of the product that made U
 };
 
@@ -52,7 +51,9 @@ int launch_check_groups(const lq_groups& g, int32_t* flag, hipStream_t s);
 int launch_check_keys(const int32_t* keys, int64_t n, int32_t G, int32_t* flag, hipStream_t s);
 // `in_vec`: rows of X and of the matrices may be read in aligned 16-byte pieces.
 int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed, bool in_vec, hipStream_t s);
-int launch_adapter_product(const GroupedArgs& main, const GroupedArgs& low, int32_t dtype, bool main_vec, bool low_vec, hipStream_t s);
+// `low` makes the partial sums of U (in low.Y, `splits` of them), `u` holds U itself.
+int launch_adapter_product(const GroupedArgs& main, const GroupedArgs& low, int splits, const float* scale, void* u, int32_t dtype, bool main_vec,
+                           bool low_vec, hipStream_t s);
 int launch_grouped_gradient(const GradientArgs& a, int32_t dtype, bool in_vec, hipStream_t s);
 
 #ifdef __HIPCC__

@@ -82,7 +82,8 @@ int adapter_splits(int64_t n, int32_t k, int32_t rp, int32_t dtype) {
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), steps / 4, 16})));
 }
 
-// U [splits x n x rp] fp32, then the group of every position.
+// Workspace: 256 bytes for LQ_CHECK_FKS, partial sums of U [splits x n x rp] fp32, U [n x rp] (fp32 or two bf16 numbers), the group of
+// every position.
 size_t adapter_u_bytes(int64_t n, int32_t rp, int splits) { return round_up(static_cast<size_t>(splits) * n * rp * 4, 256); }
 
 }  // namespace
@@ -221,7 +222,7 @@ size_t lq_adapter_workspace_bytes(int64_t n, int32_t n_groups, int32_t k, int32_
       !dtype_ok(dtype))
     return 0;
   const int32_t rp = (rank + 7) / 8 * 8;
-  return 256 + adapter_u_bytes(n, rp, adapter_splits(n, k, rp, dtype)) + round_up(static_cast<size_t>(n) * 4, 256);
+  return 256 + adapter_u_bytes(n, rp, adapter_splits(n, k, rp, dtype)) + adapter_u_bytes(n, rp, 1) + round_up(static_cast<size_t>(n) * 4, 256);
 }
 
 int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W, const lq_mat* bias, const lq_stack* A,
@@ -256,8 +257,9 @@ int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W
 
   const int32_t rp = (rank + 7) / 8 * 8;
   const int splits = adapter_splits(n, k, rp, dt);
-  float* U = reinterpret_cast<float*>(static_cast<char*>(ws) + 256);
-  int32_t* group_of = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + 256 + adapter_u_bytes(n, rp, splits));
+  char* part = static_cast<char*>(ws) + 256;
+  char* U = part + adapter_u_bytes(n, rp, splits);
+  int32_t* group_of = reinterpret_cast<int32_t*>(U + adapter_u_bytes(n, rp, 1));
   const int64_t per = 16 / static_cast<int64_t>(dtype_size(dt));
 
   GroupedArgs a{};
@@ -265,18 +267,19 @@ int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W
   a.X = X->data; a.ldx = X->ld; a.K = k; a.slots = 1;
   GroupedArgs low = a;
   low.W = A->data; low.ldw = A->ld; low.sw = A->stride;
-  low.Y = U; low.ldy = rp; low.N = rank; low.n_store = rp; low.y_grouped = 1; low.y_vec = 1;
+  low.Y = part; low.ldy = rp; low.N = rank; low.n_store = rp; low.y_grouped = 1; low.y_vec = 1;
   low.split_stride = n * rp; low.gpos = group_of;
   a.W = W->data; a.ldw = W->ld;
   if (bias) { a.bias = bias->data; a.ldb = bias->ld; }
   a.Y = Y->data; a.ldy = Y->ld; a.y_bf16 = Y->dtype == LQ_BF16; a.N = l; a.n_store = l;
   a.y_vec = whole_stores(Y->data, Y->ld, Y->dtype) && (!bias || whole_stores(bias->data, bias->ld, bias->dtype));
-  a.U = U; a.u_stride = low.split_stride; a.u_splits = splits; a.rp = rp; a.rank = rank;
-  a.B = B->data; a.ldB = B->ld; a.sB = B->stride; a.scale = scale; a.group_of = group_of;
+  a.U = U; a.u_rest = n * rp; a.rp = rp; a.rank = rank;
+  a.B = B->data; a.ldB = B->ld; a.sB = B->stride; a.group_of = group_of;
   const bool x_vec = whole_pieces(X->data, X->ld, k, dt);
-  const bool main_vec = x_vec && whole_pieces(W->data, W->ld, l, dt);
+  const bool main_vec = x_vec && whole_pieces(W->data, W->ld, l, dt) && whole_pieces(B->data, B->ld, l, dt) &&
+                        (B->stride % per == 0 || groups->n_groups == 1);
   const bool low_vec = x_vec && whole_pieces(A->data, A->ld, rank, dt) && (A->stride % per == 0 || groups->n_groups == 1);
-  return launch_adapter_product(a, low, dt, main_vec, low_vec, s);
+  return launch_adapter_product(a, low, splits, scale, U, dt, main_vec, low_vec, s);
 }
 
 }  // extern "C"

@@ -48,232 +48,10 @@ __device__ __forceinline__ void store_four(void* row, int n, int valid, f32x4 v,
     }
 }
 
-template <typename T, class S, bool BT, bool DIRECT, bool ADAPT>
-__global__ __launch_bounds__(S::THREADS) void grouped_product_kernel(GroupedArgs a) {
-  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
-  typedef Operand<T, true, S::TM, S::THREADS, KBYTES> A;
-  typedef Operand<T, BT, S::TN, S::THREADS, KBYTES> B;
-  constexpr int KSTEP = A::KSTEP, EPC = A::EPC, THREADS = S::THREADS;
-  extern __shared__ __align__(1024) char lds[];
-  __shared__ int xrow[S::TM], yrow[S::TM];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-
-  RowTile tile;
-  if constexpr (ADAPT) tile = all_rows<S::TM>(a.n, blockIdx.x, a.tiles_n);
-  else tile = find_tile<S::TM>(a.off, a.G, a.n, blockIdx.x, a.tiles_n);
-  const int n0 = tile.col * S::TN;
-  if (tile.rows <= 0) return;
-
-  for (int m = tid; m < S::TM; m += THREADS) {
-    const bool in = m < tile.rows;
-    const int p = tile.first + (in ? m : tile.rows - 1);     // (behind the last row: that row again, not stored)
-    const int r = a.order ? a.order[p] : p;
-    xrow[m] = a.x_grouped ? p : r / a.slots;
-    yrow[m] = a.y_grouped ? p : r;
-    if (!ADAPT && a.gpos && in && n0 == 0 && blockIdx.y == 0) a.gpos[p] = tile.group;
-  }
-  __syncthreads();
-
-  f32x4 acc[S::MI][S::NI];
-#pragma unroll
-  for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-    for (int j = 0; j < S::NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-  const int k_first = blockIdx.y * a.steps_per_split * KSTEP;
-  const int k_end = min(a.K, k_first + a.steps_per_split * KSTEP);
-  if (tile.group >= 0 && k_first < k_end) {
-    const T* X = static_cast<const T*>(a.X);
-    const T* W = static_cast<const T*>(a.W) + tile.group * a.sw;
-    // Where this thread's pieces of either operand lie at inner index 0, and their first inner index.  Columns behind the
-    // last one repeat the last piece (direct copies) or are zeros; they are not stored.
-    const T *pa[A::PER], *pb[B::PER];
-    int va[A::PER], vb[B::PER];
-#pragma unroll
-    for (int i = 0; i < A::PER; ++i) {
-      va[i] = A::piece_of(i) * EPC;
-      pa[i] = X + xrow[A::line_of(i)] * a.ldx + va[i];
-    }
-#pragma unroll
-    for (int i = 0; i < B::PER; ++i) {
-      const int line = B::line_of(i), e = B::piece_of(i) * EPC;
-      vb[i] = BT ? e : line;
-      pb[i] = BT ? W + static_cast<int64_t>(min(n0 + line, a.N - 1)) * a.ldw + e : W + line * a.ldw + (DIRECT ? min(n0 + e, a.N - EPC) : n0 + e);
-    }
-    const int64_t step_b = BT ? 1 : a.ldw;     // elements per inner index
-    constexpr int BUFFER = A::BYTES + B::BYTES;
-
-    if constexpr (DIRECT) {
-      auto issue = [&](int step, unsigned int to) {
-        const int k0 = k_first + step * KSTEP;
-        to += wave * 1024;
-        if (k0 + KSTEP <= k_end) {
-#pragma unroll
-          for (int i = 0; i < A::PER; ++i) copy_to_lds(pa[i] + k0, to + i * THREADS * 16);
-#pragma unroll
-          for (int i = 0; i < B::PER; ++i) copy_to_lds(pb[i] + k0 * step_b, to + A::BYTES + i * THREADS * 16);
-        } else {
-#pragma unroll
-          for (int i = 0; i < A::PER; ++i)
-            copy_to_lds(k0 + va[i] < k_end ? static_cast<const void*>(pa[i] + k0) : &g_zeros, to + i * THREADS * 16);
-#pragma unroll
-          for (int i = 0; i < B::PER; ++i)
-            copy_to_lds(k0 + vb[i] < k_end ? static_cast<const void*>(pb[i] + k0 * step_b) : &g_zeros, to + A::BYTES + i * THREADS * 16);
-        }
-      };
-      const int steps = (k_end - k_first + KSTEP - 1) / KSTEP;
-      if constexpr (THREADS == 512) {
-        multiply_in_turns<T, S, A, B>(lds, steps, issue, acc);
-      } else {
-        issue(0, lds_address(lds));
-        for (int step = 0; step < steps; ++step) {
-          const int at = (step & 1) * BUFFER;
-          meet_after_copies();     // this buffer is whole, the other one is read to its end
-          if (step + 1 < steps) issue(step + 1, lds_address(lds) + (at ^ BUFFER));
-          multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc);
-        }
-      }
-      __syncthreads();
-    } else {
-      u32x4 ra[A::PER], rb[B::PER];
-      auto fetch = [&](int k0) {
-#pragma unroll
-        for (int i = 0; i < A::PER; ++i) ra[i] = load_piece(pa[i] + k0, k_end - (k0 + va[i]));
-#pragma unroll
-        for (int i = 0; i < B::PER; ++i)
-          rb[i] = load_piece(pb[i] + k0 * step_b, BT ? k_end - (k0 + vb[i]) : k0 + vb[i] < k_end ? a.N - n0 - B::piece_of(i) * EPC : 0);
-      };
-      auto put = [&](char* to) {
-#pragma unroll
-        for (int i = 0; i < A::PER; ++i) *reinterpret_cast<u32x4*>(to + (i * THREADS + tid) * 16) = ra[i];
-#pragma unroll
-        for (int i = 0; i < B::PER; ++i) *reinterpret_cast<u32x4*>(to + A::BYTES + (i * THREADS + tid) * 16) = rb[i];
-      };
-      fetch(k_first);
-      put(lds);
-      int at = 0;
-      for (int k0 = k_first; k0 < k_end; k0 += KSTEP, at ^= BUFFER) {
-        __syncthreads();     // this buffer is whole, the other one is read to its end
-        if (k0 + KSTEP < k_end) fetch(k0 + KSTEP);
-        multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc);
-        if (k0 + KSTEP < k_end) put(lds + (at ^ BUFFER));
-      }
-      __syncthreads();
-    }
-  }
-
-  if constexpr (ADAPT) {
-    // The adapters of the tile: positions are sorted by group, so a row starts one where its group differs from the
-    // row's before it.
-    __shared__ int which[S::TM], gid[S::TM], firsts[S::TM / 64 + 1];
-    bool starts = false;
-    int g = -1;
-    if (tid < S::TM) {
-      const int p = tile.first + tid;
-      g = tid < tile.rows ? a.group_of[p] : -1;
-      starts = g >= 0 && (tid == 0 || a.group_of[p - 1] != g);
-      const unsigned long long mask = __ballot(starts);
-      which[tid] = __popcll(mask & (~0ull >> (63 - lane)));
-      if (lane == 0) firsts[tid >> 6] = __popcll(mask);
-    }
-    __syncthreads();
-    int count = 0, before = 0;
-#pragma unroll
-    for (int w = 0; w < S::TM / 64; ++w) {
-      before += w < wave ? firsts[w] : 0;
-      count += firsts[w];
-    }
-    if (tid < S::TM) {
-      const int at = which[tid] + before - 1;
-      which[tid] = g >= 0 ? at : -1;
-      if (starts) gid[at] = g;
-    }
-    __syncthreads();
-    // Four groups of 8 ranks a step: pieces 0..3 of a line of U's leading bf16 parts, 4..7 of the rest (fp32: 8 pieces).
-    constexpr bool H = sizeof(T) == 2;
-    const int per = a.rp >> 3, pieces = count * per;
-    const T* Bm = static_cast<const T*>(a.B);
-    // (only >= 0: of that adapter alone.)  True where B holds an infinity or a NaN.
-    auto stage = [&](int q0, int only) {
-      for (int id = tid; id < S::TM * (H ? 4 : 8); id += THREADS) {
-        const int m = id / (H ? 4 : 8), c = id % (H ? 4 : 8);
-        const int q = q0 + (H ? c : c >> 1), ad = q / per, r0 = (q % per) * 8 + (H ? 0 : 4 * (c & 1));
-        float u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (q < pieces && which[m] == ad && (only < 0 || only == ad)) {
-          const float* p = a.U + static_cast<int64_t>(tile.first + m) * a.rp + r0;
-          for (int z = 0; z < a.u_splits; ++z)
-#pragma unroll
-            for (int e = 0; e < (H ? 8 : 4); ++e) u[e] += p[z * a.u_stride + e];
-          const float s = a.scale ? a.scale[gid[ad]] : 1.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) u[e] = r0 + e < a.rank ? u[e] * s : 0.f;    // (0 * infinity behind the last rank)
-        }
-        if constexpr (H) {
-          u32x4 hi, lo;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            hi[e] = f32x2_to_bf16x2(u[2 * e], u[2 * e + 1]);
-            const float h0 = __uint_as_float(hi[e] << 16), h1 = __uint_as_float(hi[e] & 0xffff0000u);
-            // (an infinity leaves nothing)
-            lo[e] = f32x2_to_bf16x2(__builtin_isfinite(h0) ? u[2 * e] - h0 : 0.f, __builtin_isfinite(h1) ? u[2 * e + 1] - h1 : 0.f);
-          }
-          *reinterpret_cast<u32x4*>(lds + A::place(m, c)) = hi;
-          *reinterpret_cast<u32x4*>(lds + A::place(m, c + 4)) = lo;
-        } else {
-          *reinterpret_cast<u32x4*>(lds + A::place(m, c)) =
-              u32x4{__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3])};
-        }
-      }
-      bool bad = false;
-      for (int id = tid; id < 32 * B::CPL; id += THREADS) {
-        const int line = id / B::CPL, c = id % B::CPL;
-        const int q = q0 + (line >> 3), ad = q / per, rank = (q % per) * 8 + (line & 7);
-        u32x4 v = {0, 0, 0, 0};
-        if (q < pieces && rank < a.rank && (only < 0 || only == ad))
-          v = load_piece(Bm + gid[ad] * a.sB + rank * a.ldB + n0 + c * EPC, a.N - n0 - c * EPC);
-        constexpr unsigned int ALL = H ? 0x7f80u : 0x7f800000u;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bad |= (v[e] & ALL) == ALL || (H && (v[e] >> 16 & ALL) == ALL);
-        *reinterpret_cast<u32x4*>(lds + A::BYTES + B::place(line, c)) = v;
-      }
-      return bad;
-    };
-    const int m0 = (wave / S::WAVES_N) * S::MI * 16, c0 = (wave % S::WAVES_N) * S::NI * 16;
-    for (int q0 = 0; q0 < pieces; q0 += 4) {
-      if (!__syncthreads_or(stage(q0, -1))) {
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-          for (int j = 0; j < S::NI; ++j) {
-            const u32x4 b = B::fragment(lds + A::BYTES, c0 + 16 * j, H ? 0 : kk);
-#pragma unroll
-            for (int i = 0; i < S::MI; ++i) acc[i][j] = multiply<T>(b, A::fragment(lds, m0 + 16 * i, kk), acc[i][j]);
-          }
-      } else {
-        // An infinity or a NaN times the zeros of another adapter's rows would be a NaN there: one adapter at a time,
-        // added to its own rows only.
-        for (int ad = q0 / per; ad <= min(q0 + 3, pieces - 1) / per; ++ad) {
-          __syncthreads();
-          stage(q0, ad);
-          __syncthreads();
-          for (int j = 0; j < S::NI; ++j)
-#pragma unroll
-            for (int i = 0; i < S::MI; ++i) {
-              f32x4 part = {0.f, 0.f, 0.f, 0.f};
-              for (int kk = 0; kk < 2; ++kk)
-                part = multiply<T>(B::fragment(lds + A::BYTES, c0 + 16 * j, H ? 0 : kk), A::fragment(lds, m0 + 16 * i, kk), part);
-              const bool mine = which[m0 + 16 * i + (lane & 15)] == ad;
-#pragma unroll
-              for (int jj = 0; jj < S::NI; ++jj)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) acc[i][jj][q] += mine && jj == j ? part[q] : 0.f;
-            }
-        }
-      }
-      __syncthreads();
-    }
-  }
-
+// Bias, ReLU and gate, and the rows m of the tile for which stored(m).
+template <typename T, class S, typename F>
+__device__ __forceinline__ void store_tile(const GroupedArgs& a, const RowTile& tile, int n0, const int* yrow, f32x4 (&acc)[S::MI][S::NI], F&& stored) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = (wave / S::WAVES_N) * S::MI * 16, wn = n0 + (wave % S::WAVES_N) * S::NI * 16;
   const bool has_bias = a.bias && tile.group >= 0;
   const T* bias = static_cast<const T*>(a.bias) + (has_bias ? tile.group * a.ldb : 0);
@@ -295,7 +73,7 @@ __global__ __launch_bounds__(S::THREADS) void grouped_product_kernel(GroupedArgs
         exchange(v[0][q], v[1][q], v[2][q], v[3][q]);
       }
       const int m = wm + 16 * i + (lane & 15);
-      if (m >= tile.rows) continue;
+      if (m >= tile.rows || !stored(m)) continue;
       const int64_t r = yrow[m];
       f32x4 y[4];
 #pragma unroll
@@ -335,7 +113,7 @@ __global__ __launch_bounds__(S::THREADS) void grouped_product_kernel(GroupedArgs
 #pragma unroll
     for (int i = 0; i < S::MI; ++i) {
       const int m = wm + 16 * i + (lane & 15);
-      if (m >= tile.rows) continue;
+      if (m >= tile.rows || !stored(m)) continue;
       const int64_t r = yrow[m];
       f32x4 v = acc[i][j] + bv;
       if (a.relu)
@@ -347,6 +125,214 @@ __global__ __launch_bounds__(S::THREADS) void grouped_product_kernel(GroupedArgs
         for (int q = 0; q < 4; ++q) v[q] = h[q] > 0.f ? v[q] : 0.f;
       }
       store_four(Y + r * a.ldy * (a.y_bf16 ? 2 : 4), n, valid, v, a.y_bf16, vec);
+    }
+  }
+}
+
+template <typename T, class S, bool BT, bool DIRECT, bool ADAPT>
+__global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedArgs a) {
+  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
+  typedef Operand<T, true, S::TM, S::THREADS, KBYTES> A;
+  typedef Operand<T, BT, S::TN, S::THREADS, KBYTES> B;
+  constexpr int KSTEP = A::KSTEP, EPC = A::EPC, THREADS = S::THREADS;
+  extern __shared__ __align__(1024) char lds[];
+  __shared__ int xrow[S::TM], yrow[S::TM];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  RowTile tile;
+  if constexpr (ADAPT) tile = all_rows<S::TM>(a.n, blockIdx.x, a.tiles_n);
+  else tile = find_tile<S::TM>(a.off, a.G, a.n, blockIdx.x, a.tiles_n);
+  const int n0 = tile.col * S::TN;
+  if (tile.rows <= 0) return;
+
+  for (int m = tid; m < S::TM; m += THREADS) {
+    const bool in = m < tile.rows;
+    const int p = tile.first + (in ? m : tile.rows - 1);     // (behind the last row: that row again, not stored)
+    const int r = a.order ? a.order[p] : p;
+    xrow[m] = a.x_grouped ? p : r / a.slots;
+    yrow[m] = a.y_grouped ? p : r;
+    if (!ADAPT && a.gpos && in && n0 == 0 && blockIdx.y == 0) a.gpos[p] = tile.group;
+  }
+  __syncthreads();
+
+  // The adapters of the tile: positions are sorted by group, so a row starts one where its group differs from the one
+  // before it.  which[m]: the row's adapter, counted from the tile's first one, -1 for none.
+  __shared__ int which[ADAPT ? S::TM : 1], gid[ADAPT ? S::TM : 1], firsts[S::TM / 64];
+  int adapters = 0;
+  if constexpr (ADAPT) {
+    bool starts = false;
+    int g = -1, upto = 0;
+    if (tid < S::TM) {
+      const int p = tile.first + tid;
+      g = tid < tile.rows ? a.group_of[p] : -1;
+      starts = g >= 0 && (tid == 0 || a.group_of[p - 1] != g);
+      const unsigned long long mask = __ballot(starts);
+      upto = __popcll(mask & (~0ull >> (63 - lane)));
+      if (lane == 0) firsts[tid >> 6] = __popcll(mask);
+    }
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int w = 0; w < S::TM / 64; ++w) {
+      before += w < wave ? firsts[w] : 0;
+      adapters += firsts[w];
+    }
+    adapters = __builtin_amdgcn_readfirstlane(adapters);
+    if (tid < S::TM) {
+      which[tid] = g >= 0 ? before + upto - 1 : -1;
+      if (starts) gid[before + upto - 1] = g;
+    }
+    __syncthreads();
+  }
+
+  const int k_first = blockIdx.y * a.steps_per_split * KSTEP;
+  const int k_end = min(a.K, k_first + a.steps_per_split * KSTEP);
+  const bool any = tile.group >= 0 && k_first < k_end;
+  const T* X = static_cast<const T*>(a.X);
+  const T* W = static_cast<const T*>(a.W) + (any ? tile.group * a.sw : 0);
+  // Where this thread's pieces of either operand lie at inner index 0, and their first inner index.  Columns behind the
+  // last one repeat the last piece (direct copies) or are zeros; they are not stored.
+  const T *pa[A::PER], *pb[B::PER];
+  int va[A::PER], vb[B::PER];
+#pragma unroll
+  for (int i = 0; i < A::PER; ++i) {
+    va[i] = A::piece_of(i) * EPC;
+    pa[i] = X + xrow[A::line_of(i)] * a.ldx + va[i];
+  }
+#pragma unroll
+  for (int i = 0; i < B::PER; ++i) {
+    const int line = B::line_of(i), e = B::piece_of(i) * EPC;
+    vb[i] = BT ? e : line;
+    pb[i] = BT ? W + static_cast<int64_t>(min(n0 + line, a.N - 1)) * a.ldw + e : W + line * a.ldw + (DIRECT ? min(n0 + e, a.N - EPC) : n0 + e);
+  }
+  const int64_t step_b = BT ? 1 : a.ldw;     // elements per inner index
+  constexpr int BUFFER = A::BYTES + B::BYTES, SLOTS = KSTEP / EPC;
+  const int own_steps = any ? (k_end - k_first + KSTEP - 1) / KSTEP : 0;
+  // The adapters' steps: pieces of EPC inner indexes, two for every 8 ranks of every adapter: bf16: U's leading part and the
+  // rest of it, times the same ranks of B; fp32: the two halves of the 8.
+  const int per = ADAPT ? a.rp >> 3 : 1;
+  const int steps = own_steps + (ADAPT ? (2 * adapters * per + SLOTS - 1) / SLOTS : 0);
+  int only = -1;      // >= 0: of this adapter's pieces alone
+  auto piece_of_u = [&](int step, int i) -> const void* {
+    const int qq = (step - own_steps) * SLOTS + va[i] / EPC, q = qq >> 1, ad = q / per, line = A::line_of(i);
+    if (which[line] != ad || (only >= 0 && only != ad)) return &g_zeros;
+    const int64_t at = static_cast<int64_t>(tile.first + line) * a.rp + (q - ad * per) * 8;
+    if constexpr (sizeof(T) == 2) return static_cast<const bf16_t*>(a.U) + ((qq & 1) ? a.u_rest : 0) + at;
+    else return static_cast<const float*>(a.U) + at + 4 * (qq & 1);
+  };
+  // (the row of B that is line i of the step; NULL: zeros)
+  auto row_of_b = [&](int step, int i) -> const T* {
+    const int line = B::line_of(i), qq = (step - own_steps) * SLOTS + line / EPC, q = qq >> 1, ad = q / per;
+    const int rank = (q - ad * per) * 8 + (sizeof(T) == 2 ? 0 : 4 * (qq & 1)) + line % EPC;
+    if (ad >= adapters || rank >= a.rank || (only >= 0 && only != ad)) return nullptr;
+    return static_cast<const T*>(a.B) + gid[ad] * a.sB + rank * a.ldB;
+  };
+
+  auto issue = [&](int step, unsigned int to) {
+    const int k0 = k_first + step * KSTEP;
+    to += wave * 1024;
+    if (ADAPT && step >= own_steps) {
+#pragma unroll
+      for (int i = 0; i < A::PER; ++i) copy_to_lds(piece_of_u(step, i), to + i * THREADS * 16);
+#pragma unroll
+      for (int i = 0; i < B::PER; ++i) {
+        const T* row = row_of_b(step, i);
+        copy_to_lds(row ? static_cast<const void*>(row + min(n0 + B::piece_of(i) * EPC, a.N - EPC)) : &g_zeros, to + A::BYTES + i * THREADS * 16);
+      }
+    } else if (k0 + KSTEP <= k_end) {
+#pragma unroll
+      for (int i = 0; i < A::PER; ++i) copy_to_lds(pa[i] + k0, to + i * THREADS * 16);
+#pragma unroll
+      for (int i = 0; i < B::PER; ++i) copy_to_lds(pb[i] + k0 * step_b, to + A::BYTES + i * THREADS * 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < A::PER; ++i)
+        copy_to_lds(k0 + va[i] < k_end ? static_cast<const void*>(pa[i] + k0) : &g_zeros, to + i * THREADS * 16);
+#pragma unroll
+      for (int i = 0; i < B::PER; ++i)
+        copy_to_lds(k0 + vb[i] < k_end ? static_cast<const void*>(pb[i] + k0 * step_b) : &g_zeros, to + A::BYTES + i * THREADS * 16);
+    }
+  };
+  u32x4 ra[DIRECT ? 1 : A::PER], rb[DIRECT ? 1 : B::PER];
+  auto fetch = [&](int step) {
+    const int k0 = k_first + step * KSTEP;
+    if (ADAPT && step >= own_steps) {
+#pragma unroll
+      for (int i = 0; i < A::PER; ++i) ra[i] = *static_cast<const u32x4*>(piece_of_u(step, i));
+#pragma unroll
+      for (int i = 0; i < B::PER; ++i) {
+        const T* row = row_of_b(step, i);
+        const int n = n0 + B::piece_of(i) * EPC;
+        rb[i] = load_piece(row + n, row ? a.N - n : 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < A::PER; ++i) ra[i] = load_piece(pa[i] + k0, k_end - (k0 + va[i]));
+#pragma unroll
+      for (int i = 0; i < B::PER; ++i)
+        rb[i] = load_piece(pb[i] + k0 * step_b, BT ? k_end - (k0 + vb[i]) : k0 + vb[i] < k_end ? a.N - n0 - B::piece_of(i) * EPC : 0);
+    }
+  };
+  auto put = [&](char* to) {
+#pragma unroll
+    for (int i = 0; i < A::PER; ++i) *reinterpret_cast<u32x4*>(to + (i * THREADS + tid) * 16) = ra[i];
+#pragma unroll
+    for (int i = 0; i < B::PER; ++i) *reinterpret_cast<u32x4*>(to + A::BYTES + (i * THREADS + tid) * 16) = rb[i];
+  };
+
+  for (;;) {
+    f32x4 acc[S::MI][S::NI];
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (steps > 0) {
+      if constexpr (DIRECT && THREADS == 512) {
+        multiply_in_turns<T, S, A, B>(lds, steps, issue, acc);
+      } else if constexpr (DIRECT) {
+        issue(0, lds_address(lds));
+        for (int step = 0; step < steps; ++step) {
+          const int at = (step & 1) * BUFFER;
+          meet_after_copies();     // this buffer is whole, the other one is read to its end
+          if (step + 1 < steps) issue(step + 1, lds_address(lds) + (at ^ BUFFER));
+          multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc);
+        }
+      } else {
+        fetch(0);
+        put(lds);
+        for (int step = 0; step < steps; ++step) {
+          const int at = (step & 1) * BUFFER;
+          __syncthreads();         // likewise
+          if (step + 1 < steps) fetch(step + 1);
+          multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc);
+          if (step + 1 < steps) put(lds + (at ^ BUFFER));
+        }
+      }
+    }
+    if constexpr (!ADAPT) {
+      store_tile<T, S>(a, tile, n0, yrow, acc, [](int) { return true; });
+      return;
+    } else {
+      // An infinity or a NaN in one adapter's B, times the zeros in the rows of others, is a NaN there.  A tile with a NaN
+      // is therefore computed again for one adapter at a time (the last time for the rows without one) and stored for its
+      // rows only: the same sums, with zeros for the other adapters' terms.
+      if (only < 0) {
+        bool nan = false;
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+          for (int j = 0; j < S::NI; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) nan |= acc[i][j][q] != acc[i][j][q];
+        if (!__syncthreads_or(nan)) {
+          store_tile<T, S>(a, tile, n0, yrow, acc, [](int) { return true; });
+          return;
+        }
+      } else {
+        store_tile<T, S>(a, tile, n0, yrow, acc, [&](int m) { return which[m] == (only < adapters ? only : -1); });
+        __syncthreads();           // (LDS is read to its end)
+      }
+      if (++only > adapters) return;
     }
   }
 }
@@ -387,16 +373,60 @@ template <typename T> int product(const GroupedArgs& a, bool transposed, bool in
   return in_vec ? by_size<T, false, true, false>(a, splits, s) : by_size<T, false, false, false>(a, splits, s);
 }
 
+// U from the partial sums of its product: scaled, zeros behind the last rank, as two bf16 numbers beside bf16 matrices.  Eight
+// ranks of a position a thread.
+template <bool HALVES>
+__global__ __launch_bounds__(256) void adapter_scale_kernel(const float* __restrict__ part, int splits, int64_t stride, int64_t pieces, int per,
+                                                            int rank, const float* __restrict__ scale, const int32_t* __restrict__ group_of,
+                                                            void* __restrict__ out, int64_t rest) {
+  const int64_t id = blockIdx.x * 256ll + threadIdx.x;
+  if (id >= pieces) return;
+  const int r0 = static_cast<int>(id % per) * 8, g = group_of[id / per];
+  f32x4 u[2] = {};
+  for (int z = 0; z < splits; ++z)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) u[h] += *reinterpret_cast<const f32x4*>(part + z * stride + id * 8 + 4 * h);
+  const float s = scale && g >= 0 ? scale[g] : 1.f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[h][e] = g >= 0 && r0 + 4 * h + e < rank ? u[h][e] * s : 0.f;
+  if constexpr (HALVES) {
+    u32x4 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = u[e >> 1][2 * (e & 1)], y = u[e >> 1][2 * (e & 1) + 1];
+      hi[e] = f32x2_to_bf16x2(x, y);
+      const float h0 = __uint_as_float(hi[e] << 16), h1 = __uint_as_float(hi[e] & 0xffff0000u);
+      lo[e] = f32x2_to_bf16x2(__builtin_isfinite(h0) ? x - h0 : 0.f, __builtin_isfinite(h1) ? y - h1 : 0.f);    // (an infinity leaves nothing)
+    }
+    *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(out) + id * 8) = hi;
+    *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(out) + rest + id * 8) = lo;
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + id * 8 + 4 * h) = u[h];
+  }
+}
+
 }  // namespace
 
 int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed, bool in_vec, hipStream_t s) {
   return dtype == LQ_BF16 ? product<bf16_t>(a, transposed, in_vec, 1, s) : product<float>(a, transposed, in_vec, 1, s);
 }
 
-int launch_adapter_product(const GroupedArgs& m, const GroupedArgs& low, int32_t dtype, bool main_vec, bool low_vec, hipStream_t s) {
-  const int rc = dtype == LQ_BF16 ? product<bf16_t>(low, false, low_vec, m.u_splits, s) : product<float>(low, false, low_vec, m.u_splits, s);
+int launch_adapter_product(const GroupedArgs& m, const GroupedArgs& low, int splits, const float* scale, void* u, int32_t dtype, bool main_vec,
+                           bool low_vec, hipStream_t s) {
+  const bool halves = dtype == LQ_BF16;
+  const int rc = halves ? product<bf16_t>(low, false, low_vec, splits, s) : product<float>(low, false, low_vec, splits, s);
   if (rc) return rc;
-  if (dtype == LQ_BF16) return main_vec ? by_size<bf16_t, false, true, true>(m, 1, s) : by_size<bf16_t, false, false, true>(m, 1, s);
+  const int per = m.rp / 8;
+  const int64_t pieces = static_cast<int64_t>(m.n) * per;
+  const unsigned blocks = static_cast<unsigned>((pieces + 255) / 256);
+  const float* part = static_cast<const float*>(low.Y);
+  if (halves) adapter_scale_kernel<true><<<blocks, 256, 0, s>>>(part, splits, low.split_stride, pieces, per, m.rank, scale, low.gpos, u, m.u_rest);
+  else adapter_scale_kernel<false><<<blocks, 256, 0, s>>>(part, splits, low.split_stride, pieces, per, m.rank, scale, low.gpos, u, 0);
+  LQ_LAUNCH_CHECK("adapter_scale_kernel");
+  if (halves) return main_vec ? by_size<bf16_t, false, true, true>(m, 1, s) : by_size<bf16_t, false, false, true>(m, 1, s);
   return main_vec ? by_size<float, false, true, true>(m, 1, s) : by_size<float, false, false, true>(m, 1, s);
 }
 
