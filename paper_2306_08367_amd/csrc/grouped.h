@@ -43,6 +43,8 @@ struct GradientArgs {
   void* db; int64_t ldb;
   int32_t k, l;
   int32_t tiles_m, tiles_n;
+  int32_t most;          // rows of a chunk
+  float* part;           // partial sums of the chunks of groups of more than one: [chunk][k + 1][l], the last row for db
 };
 
 int launch_group_rows(const int32_t* keys, int64_t n, int32_t G, int32_t* off, int32_t* order, void* ws, hipStream_t s);
@@ -54,7 +56,8 @@ int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed,
 // `low` makes the partial sums of U (in low.Y, `splits` of them), `u` holds U itself.
 int launch_adapter_product(const GroupedArgs& main, const GroupedArgs& low, int splits, const float* scale, void* u, int32_t dtype, bool main_vec,
                            bool low_vec, hipStream_t s);
-int launch_grouped_gradient(const GradientArgs& a, int32_t dtype, bool in_vec, hipStream_t s);
+size_t grouped_gradient_ws_bytes(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype);
+int launch_grouped_gradient(const GradientArgs& a, int32_t dtype, bool in_vec, void* ws, size_t ws_bytes, hipStream_t s);
 
 #ifdef __HIPCC__
 
@@ -153,6 +156,52 @@ template <int TM> __device__ __forceinline__ RowTile all_rows(int n, int id, int
   return tile_of_range<TM>(0, 0, n, die_order(id, (n + TM - 1) / TM * cols), cols);
 }
 
+// Rows of a group are added up in chunks of `most` rows.  Chunk `t`: group, rows, and among the chunks of the groups of more than
+// one the place of this chunk's partial sums (-1: the only chunk of its group).  A group without rows has one empty chunk.
+// group < 0: there is no such chunk.  Called by a whole wavefront, like find_tile.
+struct Chunk { int group, first, rows, place; };
+__device__ __forceinline__ Chunk find_chunk(const int32_t* __restrict__ off, int G, int most, int t) {
+  const int lane = threadIdx.x & 63;
+  const int per = (G + 63) >> 6;
+  const int g0 = min(lane * per, G), g1 = min(g0 + per, G);
+  int own = 0, parts = 0;
+  for (int g = g0; g < g1; ++g) {
+    const int c = max(1, (off[g + 1] - off[g] + most - 1) / most);
+    own += c;
+    parts += c > 1 ? c : 0;
+  }
+  int upto = own, parts_upto = parts;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(upto, d), w = __shfl_up(parts_upto, d);
+    if (lane >= d) {
+      upto += v;
+      parts_upto += w;
+    }
+  }
+  const unsigned long long holds = __ballot(upto > t);
+  if (!holds) return {-1, 0, 0, -1};
+  const int at = __ffsll(static_cast<long long>(holds)) - 1;
+  int group = 0, first = 0, rows = 0, place = -1;
+  if (lane == at) {
+    int before = upto - own, parts_before = parts_upto - parts;
+    for (int g = g0; g < g1; ++g) {
+      const int b = off[g], e = off[g + 1], c = max(1, (e - b + most - 1) / most);
+      if (t < before + c) {
+        group = g;
+        first = b + (t - before) * most;
+        rows = min(most, e - first);
+        place = c > 1 ? parts_before + t - before : -1;
+        break;
+      }
+      before += c;
+      parts_before += c > 1 ? c : 0;
+    }
+  }
+  return {__builtin_amdgcn_readlane(group, at), __builtin_amdgcn_readlane(first, at), __builtin_amdgcn_readlane(rows, at),
+          __builtin_amdgcn_readlane(place, at)};
+}
+
 // One operand of the tile product in LDS: EXT rows of the result (or columns) by KSTEP of the inner dimension, as
 // lines of 16-byte pieces.
 //   KMAJ    a line per row, the inner dimension along it (KBYTES bytes): a lane's operand is one 16-byte read
@@ -228,9 +277,9 @@ template <int TM_, int TN_, int WAVES_M_, int WAVES_N_> struct TileShape {
   static constexpr int MI = TM / WAVES_M / 16, NI = TN / WAVES_N / 16;
 };
 
-// One step of the product of a wavefront's part of the tile.
-template <typename T, class S, class A, class B>
-__device__ __forceinline__ void multiply_step(const char* la, const char* lb, f32x4 (&acc)[S::MI][S::NI]) {
+// One step of the product of a wavefront's part of the tile; with_b(b): called with its operands of B, twice.
+template <typename T, class S, class A, class B, typename H>
+__device__ __forceinline__ void multiply_step(const char* la, const char* lb, f32x4 (&acc)[S::MI][S::NI], H&& with_b) {
   const int wave = threadIdx.x >> 6;
   const int m0 = (wave / S::WAVES_N) * S::MI * 16, n0 = (wave % S::WAVES_N) * S::NI * 16;
 #pragma unroll
@@ -244,6 +293,7 @@ __device__ __forceinline__ void multiply_step(const char* la, const char* lb, f3
     for (int i = 0; i < S::MI; ++i)
 #pragma unroll
       for (int j = 0; j < S::NI; ++j) acc[i][j] = multiply<T>(b[j], a[i], acc[i][j]);
+    with_b(b);
   }
 }
 
@@ -273,8 +323,9 @@ __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 // last readers are the second four in turn 2 u - 1: each wavefront issues its copies for it when it begins to read block u,
 // and waits for its copies of block u + 1 at the end of turn 2 u + 1, with those of two blocks still in flight: they have
 // five or six turns to arrive.
-template <typename T, class S, class A, class B, typename F>
-__device__ __forceinline__ void multiply_in_turns(char* lds, int units, F&& issue, f32x4 (&acc)[S::MI][S::NI]) {
+// with_b(b): called with the wavefront's operands of B beside the products.
+template <typename T, class S, class A, class B, typename F, typename H>
+__device__ __forceinline__ void multiply_in_turns(char* lds, int units, F&& issue, f32x4 (&acc)[S::MI][S::NI], H&& with_b) {
   static_assert(S::THREADS == 512 && S::WAVES_N == 4, "two wavefronts a SIMD");
   constexpr int BLOCK = A::BYTES + B::BYTES, COPIES = A::PER + B::PER;
   static_assert(COPIES == 4, "the waits below count copies");
@@ -312,6 +363,7 @@ __device__ __forceinline__ void multiply_in_turns(char* lds, int units, F&& issu
     for (int i = 0; i < S::MI; ++i)
 #pragma unroll
       for (int j = 0; j < S::NI; ++j) acc[i][j] = multiply<T>(b[j], a[i], acc[i][j]);
+    with_b(b);
     __builtin_amdgcn_s_setprio(0);
     if (!second) wait_copies(u + 3 < units);
     turn();

@@ -125,8 +125,8 @@ size_t lq_grouped_workspace_bytes(int64_t n, int32_t n_groups, int32_t k, int32_
   return 0;
 }
 size_t lq_grouped_gradient_workspace_bytes(int64_t n, int32_t n_groups, int32_t k, int32_t l, int32_t dtype) {
-  (void)n; (void)n_groups; (void)k; (void)l; (void)dtype;
-  return 0;
+  if (n < 0 || n > MAX_POSITIONS || n_groups < 1 || n_groups > LQ_MAX_MODELS || k < 1 || l < 1 || !dtype_ok(dtype)) return 0;
+  return grouped_gradient_ws_bytes(n, n_groups, k, l, dtype);
 }
 
 int lq_grouped_product(const lq_groups* groups, const lq_mat* X, int32_t x_slots, const lq_stack* W, const lq_mat* bias,
@@ -214,7 +214,8 @@ int lq_grouped_gradient(const lq_groups* groups, const lq_mat* X, int32_t x_slot
   if (db) { a.db = db->data; a.ldb = db->ld; }
   a.k = X->cols; a.l = dY->cols;
   const bool in_vec = whole_pieces(X->data, X->ld, X->cols, X->dtype) && whole_pieces(dY->data, dY->ld, dY->cols, X->dtype);
-  return launch_grouped_gradient(a, X->dtype, in_vec, s);
+  if (ws && !aligned(ws, 256)) return fail(LQ_ERR_WORKSPACE, "lq_grouped_gradient: the workspace is not 256-byte aligned");
+  return launch_grouped_gradient(a, X->dtype, in_vec, ws, ws_bytes, s);
 }
 
 size_t lq_adapter_workspace_bytes(int64_t n, int32_t n_groups, int32_t k, int32_t l, int32_t rank, int32_t dtype) {

@@ -2,24 +2,49 @@
 //
 // A tile of dW_g is a product whose inner dimension is the group's rows: both operands are lines of the inner index
 // (a row of X, a row of dY), so bf16 ones come transposed out of LDS.  The bias is the product of ones with dY, in the
-// workgroups of the first rows of the tiles.
+// wavefronts of the first rows of the first tiles.
+//
+// Groups differ in size and only the device knows by how much, so a group's rows are added up in chunks of at most `most`
+// rows, each by workgroups of its own.  A group of one chunk is written at once; the chunks of a larger one leave partial
+// sums in the workspace, which a second launch adds up in their order: no atomics, the same bits every time.  `most` is
+// half of what a workgroup would get if all rows were shared out evenly, but no fewer rows than make up for the partial
+// sums' way through memory.
 #include "grouped.h"
 
 namespace lq {
 namespace {
 
+template <bool BF16> __device__ __forceinline__ void store_values(void* base, int64_t at, int valid, bool vec, f32x4 v) {
+  if (vec && valid >= 4) {
+    if constexpr (BF16) *reinterpret_cast<uint2*>(static_cast<bf16_t*>(base) + at) = uint2{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
+    else *reinterpret_cast<f32x4*>(static_cast<float*>(base) + at) = v;
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (q < valid) {
+      if constexpr (BF16) static_cast<bf16_t*>(base)[at + q] = f32_to_bf16(v[q]);
+      else static_cast<float*>(base)[at + q] = v[q];
+    }
+}
+
+constexpr int SEGMENT = 4096;     // rows whose numbers are held in LDS at a time
+
 template <typename T, class S, bool DIRECT>
-__global__ __launch_bounds__(S::THREADS) void grouped_gradient_kernel(GradientArgs a) {
-  typedef Operand<T, false, S::TM, S::THREADS> A;
-  typedef Operand<T, false, S::TN, S::THREADS> B;
-  constexpr int KSTEP = A::KSTEP, EPC = A::EPC, THREADS = S::THREADS;
+__global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(GradientArgs a) {
+  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
+  typedef Operand<T, false, S::TM, S::THREADS, KBYTES> A;
+  typedef Operand<T, false, S::TN, S::THREADS, KBYTES> B;
+  constexpr int KSTEP = A::KSTEP, EPC = A::EPC, THREADS = S::THREADS, BUFFER = A::BYTES + B::BYTES;
   extern __shared__ __align__(1024) char lds[];
+  __shared__ int row[SEGMENT];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tiles = a.tiles_m * a.tiles_n;
   const int id = die_order(blockIdx.x, gridDim.x);
-  const int per_group = a.tiles_m * a.tiles_n;
-  const int group = id / per_group, tm = id % per_group / a.tiles_n, tn = id % a.tiles_n;
+  const Chunk chunk = find_chunk(a.off, a.G, a.most, id / tiles);
+  if (chunk.group < 0) return;
+  const int tm = id % tiles / a.tiles_n, tn = id % tiles % a.tiles_n;
   const int m0 = tm * S::TM, n0 = tn * S::TN;
-  const int first = a.off[group], rows = a.off[group + 1] - first;
 
   f32x4 acc[S::MI][S::NI], sum[S::NI];
 #pragma unroll
@@ -32,86 +57,88 @@ __global__ __launch_bounds__(S::THREADS) void grouped_gradient_kernel(GradientAr
   const bool bias = a.db && tm == 0 && wm == 0;
   const unsigned int one = sizeof(T) == 2 ? 0x3f803f80u : 0x3f800000u;
   const u32x4 ones = {one, one, one, one};
+  const auto add_up = [&](const u32x4(&b)[S::NI]) {
+    if (bias)
+#pragma unroll
+      for (int j = 0; j < S::NI; ++j) sum[j] = multiply<T>(b[j], ones, sum[j]);
+  };
 
+  // (columns behind the last one repeat the last piece (direct copies) or are zeros; they are not stored)
   const T *X = static_cast<const T*>(a.X), *dY = static_cast<const T*>(a.dY);
-  // The rows of X and dY that hold this thread's pieces of the step from k0 on (-1: none).
-  auto row_of = [&](int k, bool grouped, int slots) -> int {
-    if (k >= rows) return -1;
-    const int p = first + k;
-    return grouped || !a.order ? (grouped ? p : p / slots) : a.order[p] / slots;
-  };
-  int xr[A::PER], yr[B::PER];
-  auto look_up = [&](int k0) {
+  int ca[A::PER], cb[B::PER];
 #pragma unroll
-    for (int i = 0; i < A::PER; ++i) xr[i] = row_of(k0 + A::line_of(i), a.x_grouped, a.slots);
+  for (int i = 0; i < A::PER; ++i) ca[i] = DIRECT ? min(m0 + A::piece_of(i) * EPC, a.k - EPC) : m0 + A::piece_of(i) * EPC;
 #pragma unroll
-    for (int i = 0; i < B::PER; ++i) yr[i] = row_of(k0 + B::line_of(i), a.y_grouped, 1);
-  };
-  u32x4 ra[DIRECT ? 1 : A::PER], rb[DIRECT ? 1 : B::PER];
-  auto fetch = [&](char* to) {
-    const unsigned int at = DIRECT ? lds_address(to) : 0;
+  for (int i = 0; i < B::PER; ++i) cb[i] = DIRECT ? min(n0 + B::piece_of(i) * EPC, a.l - EPC) : n0 + B::piece_of(i) * EPC;
+
+  for (int s0 = 0; s0 < chunk.rows; s0 += SEGMENT) {
+    const int first = chunk.first + s0, rows = min(SEGMENT, chunk.rows - s0), steps = (rows + KSTEP - 1) / KSTEP;
+    __syncthreads();     // (the segment before is read to its end)
+    for (int i = tid; i < rows; i += THREADS) row[i] = a.order ? a.order[first + i] : first + i;
+    __syncthreads();
+    auto x_row = [&](int line) { return X + static_cast<int64_t>(a.x_grouped ? first + line : row[line] / a.slots) * a.ldx; };
+    auto y_row = [&](int line) { return dY + static_cast<int64_t>(a.y_grouped ? first + line : row[line]) * a.ldy; };
+    auto issue = [&](int step, unsigned int to) {
+      const int k0 = step * KSTEP;
+      to += wave * 1024;
+      // (rows behind the last one are zeros in both operands)
 #pragma unroll
-    for (int i = 0; i < A::PER; ++i) {
-      const int c = m0 + A::piece_of(i) * EPC;
-      const T* p = X + xr[i] * a.ldx + c;
-      if constexpr (DIRECT) copy_to_lds(xr[i] >= 0 && c < a.k ? static_cast<const void*>(p) : &g_zeros, at + (i * THREADS + wave * 64) * 16);
-      else ra[i] = load_piece(p, xr[i] >= 0 ? a.k - c : 0);
-    }
-#pragma unroll
-    for (int i = 0; i < B::PER; ++i) {
-      const int c = n0 + B::piece_of(i) * EPC;
-      const T* p = dY + yr[i] * a.ldy + c;
-      if constexpr (DIRECT) copy_to_lds(yr[i] >= 0 && c < a.l ? static_cast<const void*>(p) : &g_zeros, at + A::BYTES + (i * THREADS + wave * 64) * 16);
-      else rb[i] = load_piece(p, yr[i] >= 0 ? a.l - c : 0);
-    }
-  };
-  auto put = [&](char* to) {
-    if constexpr (!DIRECT) {
-#pragma unroll
-      for (int i = 0; i < A::PER; ++i) *reinterpret_cast<u32x4*>(to + (i * THREADS + tid) * 16) = ra[i];
-#pragma unroll
-      for (int i = 0; i < B::PER; ++i) *reinterpret_cast<u32x4*>(to + A::BYTES + (i * THREADS + tid) * 16) = rb[i];
-    }
-  };
-  constexpr int BUFFER = A::BYTES + B::BYTES;
-  if (rows > 0) {
-    look_up(0);
-    fetch(lds);
-    put(lds);
-    look_up(KSTEP);
-    int at = 0;
-    for (int k0 = 0; k0 < rows; k0 += KSTEP, at ^= 1) {
-      if constexpr (DIRECT) meet_after_copies();
-      else __syncthreads();     // this buffer is whole, the other one is read to its end
-      const bool more = k0 + KSTEP < rows;
-      if (more) {
-        fetch(lds + (at ^ 1) * BUFFER);
-        look_up(k0 + 2 * KSTEP);
+      for (int i = 0; i < A::PER; ++i) {
+        const int line = k0 + A::line_of(i);
+        copy_to_lds(line < rows ? static_cast<const void*>(x_row(line) + ca[i]) : &g_zeros, to + i * THREADS * 16);
       }
-      multiply_step<T, S, A, B>(lds + at * BUFFER, lds + at * BUFFER + A::BYTES, acc);
-      if (bias) {
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-          for (int j = 0; j < S::NI; ++j) sum[j] = multiply<T>(B::fragment(lds + at * BUFFER + A::BYTES, wn + 16 * j, kk), ones, sum[j]);
+      for (int i = 0; i < B::PER; ++i) {
+        const int line = k0 + B::line_of(i);
+        copy_to_lds(line < rows ? static_cast<const void*>(y_row(line) + cb[i]) : &g_zeros, to + A::BYTES + i * THREADS * 16);
       }
-      if (more) put(lds + (at ^ 1) * BUFFER);
+    };
+    if constexpr (DIRECT && THREADS == 512) {
+      multiply_in_turns<T, S, A, B>(lds, steps, issue, acc, add_up);
+    } else if constexpr (DIRECT) {
+      issue(0, lds_address(lds));
+      for (int step = 0; step < steps; ++step) {
+        const int at = (step & 1) * BUFFER;
+        meet_after_copies();     // this buffer is whole, the other one is read to its end
+        if (step + 1 < steps) issue(step + 1, lds_address(lds) + (at ^ BUFFER));
+        multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc, add_up);
+      }
+    } else {
+      u32x4 ra[A::PER], rb[B::PER];
+      auto fetch = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < A::PER; ++i) {
+          const int line = step * KSTEP + A::line_of(i);
+          ra[i] = line < rows ? load_piece(x_row(line) + ca[i], a.k - ca[i]) : u32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < B::PER; ++i) {
+          const int line = step * KSTEP + B::line_of(i);
+          rb[i] = line < rows ? load_piece(y_row(line) + cb[i], a.l - cb[i]) : u32x4{0, 0, 0, 0};
+        }
+      };
+      auto put = [&](char* to) {
+#pragma unroll
+        for (int i = 0; i < A::PER; ++i) *reinterpret_cast<u32x4*>(to + (i * THREADS + tid) * 16) = ra[i];
+#pragma unroll
+        for (int i = 0; i < B::PER; ++i) *reinterpret_cast<u32x4*>(to + A::BYTES + (i * THREADS + tid) * 16) = rb[i];
+      };
+      fetch(0);
+      put(lds);
+      for (int step = 0; step < steps; ++step) {
+        const int at = (step & 1) * BUFFER;
+        __syncthreads();         // likewise
+        if (step + 1 < steps) fetch(step + 1);
+        multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc, add_up);
+        if (step + 1 < steps) put(lds + (at ^ BUFFER));
+      }
     }
   }
 
-  auto store = [&](void* base, int64_t row, int n, f32x4 v) {
-    const int valid = a.l - n;
-    if (a.w_vec && valid >= 4) {
-      if (a.w_bf16) *reinterpret_cast<uint2*>(static_cast<bf16_t*>(base) + row + n) = uint2{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
-      else *reinterpret_cast<f32x4*>(static_cast<float*>(base) + row + n) = v;
-      return;
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (q < valid) {
-        if (a.w_bf16) static_cast<bf16_t*>(base)[row + n + q] = f32_to_bf16(v[q]);
-        else static_cast<float*>(base)[row + n + q] = v[q];
-      }
+  const int64_t part = chunk.place >= 0 ? chunk.place * (static_cast<int64_t>(a.k) + 1) * a.l : 0;
+  auto store = [&](void* base, int64_t at, int n, f32x4 v) {
+    if (a.w_bf16) store_values<true>(base, at + n, a.l - n, a.w_vec, v);
+    else store_values<false>(base, at + n, a.l - n, a.w_vec, v);
   };
 #pragma unroll
   for (int j = 0; j < S::NI; ++j) {
@@ -120,22 +147,108 @@ __global__ __launch_bounds__(S::THREADS) void grouped_gradient_kernel(GradientAr
 #pragma unroll
     for (int i = 0; i < S::MI; ++i) {
       const int m = m0 + wm + 16 * i + (lane & 15);
-      if (m < a.k) store(a.dW, group * a.sw + m * a.ldw, n, acc[i][j]);
+      if (m >= a.k) continue;
+      if (chunk.place >= 0) store_values<false>(a.part, part + static_cast<int64_t>(m) * a.l + n, a.l - n, (a.l & 3) == 0, acc[i][j]);
+      else store(a.dW, chunk.group * a.sw + m * a.ldw, n, acc[i][j]);
     }
-    if (bias && (lane & 15) == 0) store(a.db, group * a.ldb, n, sum[j]);
+    if (bias && (lane & 15) == 0) {
+      if (chunk.place >= 0) store_values<false>(a.part, part + static_cast<int64_t>(a.k) * a.l + n, a.l - n, (a.l & 3) == 0, sum[j]);
+      else store(a.db, chunk.group * a.ldb, n, sum[j]);
+    }
   }
 }
 
-template <typename T, class S, bool DIRECT> int launch(GradientArgs a, hipStream_t s) {
-  typedef Operand<T, false, S::TM, S::THREADS> A;
-  typedef Operand<T, false, S::TN, S::THREADS> B;
-  constexpr int LDS = 2 * (A::BYTES + B::BYTES);
+// Adds up the partial sums of the blockIdx.y-th group of more than one chunk, four results of a row a thread.
+template <bool BF16> __global__ __launch_bounds__(256) void gradient_sum_kernel(GradientArgs a) {
+  const int lane = threadIdx.x & 63;
+  // the group, and how many partial sums lie before its own
+  const int per = (a.G + 63) >> 6, g0 = min(lane * per, a.G), g1 = min(g0 + per, a.G);
+  int own = 0, parts = 0;
+  for (int g = g0; g < g1; ++g) {
+    const int c = (a.off[g + 1] - a.off[g] + a.most - 1) / a.most;
+    own += c > 1;
+    parts += c > 1 ? c : 0;
+  }
+  int upto = own, parts_upto = parts;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(upto, d), w = __shfl_up(parts_upto, d);
+    if (lane >= d) {
+      upto += v;
+      parts_upto += w;
+    }
+  }
+  const int which = blockIdx.y;
+  const unsigned long long holds = __ballot(upto > which);
+  if (!holds) return;
+  const int at = __ffsll(static_cast<long long>(holds)) - 1;
+  int group = 0, first = 0, count = 0;
+  if (lane == at) {
+    int left = which - (upto - own);
+    first = parts_upto - parts;
+    for (int g = g0; g < g1; ++g) {
+      const int c = (a.off[g + 1] - a.off[g] + a.most - 1) / a.most;
+      if (c <= 1) continue;
+      if (left-- == 0) {
+        group = g;
+        count = c;
+        break;
+      }
+      first += c;
+    }
+  }
+  group = __builtin_amdgcn_readlane(group, at);
+  first = __builtin_amdgcn_readlane(first, at);
+  count = __builtin_amdgcn_readlane(count, at);
+
+  const int fours = (a.l + 3) >> 2, rows = a.k + (a.db ? 1 : 0);
+  const int64_t stride = (static_cast<int64_t>(a.k) + 1) * a.l;
+  for (int64_t id = blockIdx.x * 256ll + threadIdx.x; id < static_cast<int64_t>(rows) * fours; id += gridDim.x * 256ll) {
+    const int m = static_cast<int>(id / fours), n = static_cast<int>(id - static_cast<int64_t>(m) * fours) * 4;
+    const float* p = a.part + first * stride + static_cast<int64_t>(m) * a.l + n;
+    const int valid = min(4, a.l - n);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if ((a.l & 3) == 0) {
+      for (int c = 0; c < count; ++c) v += *reinterpret_cast<const f32x4*>(p + c * stride);
+    } else {
+      for (int c = 0; c < count; ++c)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (q < valid) v[q] += p[c * stride + q];
+    }
+    if (m < a.k) store_values<BF16>(a.dW, group * a.sw + m * a.ldw + n, valid, a.w_vec, v);
+    else store_values<BF16>(a.db, group * a.ldb + n, valid, a.w_vec, v);
+  }
+}
+
+// Side of the tiles and most rows of a chunk.  Large tiles read less from LDS for an instruction: 256 from where most of a tile
+// is filled, in bf16 with aligned rows.  A workgroup's share of n rows is n * tiles / workgroups that run at once (one of 512
+// threads a compute unit, else two).
+struct Plan { int side; int64_t most, places; };
+Plan plan_of(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype, bool in_vec) {
+  Plan p;
+  p.side = dtype == LQ_BF16 && in_vec && k > 192 && l > 192 ? 256 : k > 64 && l > 64 ? 128 : 64;
+  const int64_t tiles = static_cast<int64_t>((k + p.side - 1) / p.side) * ((l + p.side - 1) / p.side);
+  const int64_t even = n * tiles / (2 * num_cus() * (p.side == 256 ? 1 : 2));
+  p.most = std::max<int64_t>((even + 63) / 64 * 64, dtype == LQ_BF16 ? 1024 : 256);
+  // chunks of groups of more than one: fewer than two for every `most` rows, and fewer than one more a group
+  p.places = std::min<int64_t>(2 * n / p.most, n / p.most + G);
+  return p;
+}
+size_t place_bytes(int64_t places, int32_t k, int32_t l) { return static_cast<size_t>(places) * (static_cast<size_t>(k) + 1) * l * 4; }
+
+template <typename T, class S, bool DIRECT> int launch(GradientArgs a, const Plan& p, hipStream_t s) {
+  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
+  typedef Operand<T, false, S::TM, S::THREADS, KBYTES> A;
+  typedef Operand<T, false, S::TN, S::THREADS, KBYTES> B;
+  constexpr int LDS = (S::THREADS == 512 ? 4 : 2) * (A::BYTES + B::BYTES);
   a.tiles_m = (a.k + S::TM - 1) / S::TM;
   a.tiles_n = (a.l + S::TN - 1) / S::TN;
-  const int64_t blocks = static_cast<int64_t>(a.G) * a.tiles_m * a.tiles_n;
+  const int64_t chunks = a.n / p.most + a.G;
+  const int64_t blocks = chunks * a.tiles_m * a.tiles_n;
   if (blocks > 0x7fffffff) return fail(LQ_ERR_UNSUPPORTED, "grouped gradient: %lld tiles are more than one launch takes", (long long)blocks);
   const auto kernel = grouped_gradient_kernel<T, S, DIRECT>;
-  if (LDS >= 64 * 1024)
+  if (LDS + SEGMENT * 4 > 48 * 1024)
     LQ_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
   kernel<<<static_cast<unsigned>(blocks), S::THREADS, LDS, s>>>(a);
   LQ_LAUNCH_CHECK("grouped_gradient_kernel");
@@ -144,17 +257,41 @@ template <typename T, class S, bool DIRECT> int launch(GradientArgs a, hipStream
 
 typedef TileShape<128, 128, 2, 2> Tile128;
 typedef TileShape<64, 64, 2, 2> Tile64;
+typedef TileShape<256, 256, 2, 4> Tile256;
 
-template <typename T, bool DIRECT> int by_size(const GradientArgs& a, hipStream_t s) {
-  const int64_t large = static_cast<int64_t>((a.k + 127) / 128) * ((a.l + 127) / 128) * a.G;
-  return large >= num_cus() ? launch<T, Tile128, DIRECT>(a, s) : launch<T, Tile64, DIRECT>(a, s);
+template <typename T, bool DIRECT> int by_size(const GradientArgs& a, const Plan& p, hipStream_t s) {
+  if constexpr (sizeof(T) == 2 && DIRECT)
+    if (p.side == 256) return launch<T, Tile256, DIRECT>(a, p, s);
+  return p.side == 128 ? launch<T, Tile128, DIRECT>(a, p, s) : launch<T, Tile64, DIRECT>(a, p, s);
 }
 
 }  // namespace
 
-int launch_grouped_gradient(const GradientArgs& a, int32_t dtype, bool in_vec, hipStream_t s) {
-  if (dtype == LQ_BF16) return in_vec ? by_size<bf16_t, true>(a, s) : by_size<bf16_t, false>(a, s);
-  return in_vec ? by_size<float, true>(a, s) : by_size<float, false>(a, s);
+size_t grouped_gradient_ws_bytes(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype) {
+  size_t most = 0;
+  for (const bool in_vec : {false, true}) most = std::max(most, place_bytes(plan_of(n, G, k, l, dtype, in_vec).places, k, l));
+  return round_up(most, 256);
+}
+
+int launch_grouped_gradient(const GradientArgs& args, int32_t dtype, bool in_vec, void* ws, size_t ws_bytes, hipStream_t s) {
+  GradientArgs a = args;
+  Plan p = plan_of(a.n, a.G, a.k, a.l, dtype, in_vec);
+  if (!ws || ws_bytes < place_bytes(p.places, a.k, a.l)) p.most = std::max<int64_t>(a.n, 1);     // without room: whole groups
+  a.most = static_cast<int32_t>(p.most);
+  a.part = static_cast<float*>(ws);
+  int rc;
+  if (dtype == LQ_BF16) rc = in_vec ? by_size<bf16_t, true>(a, p, s) : by_size<bf16_t, false>(a, p, s);
+  else rc = in_vec ? by_size<float, true>(a, p, s) : by_size<float, false>(a, p, s);
+  if (rc) return rc;
+  if (a.n > p.most) {
+    const int64_t fours = static_cast<int64_t>(a.k + 1) * ((a.l + 3) / 4);
+    const unsigned groups = static_cast<unsigned>(std::min<int64_t>(a.G, a.n / p.most));    // more than `most` rows each
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>((fours + 255) / 256, 1024)), groups);
+    if (a.w_bf16) gradient_sum_kernel<true><<<grid, 256, 0, s>>>(a);
+    else gradient_sum_kernel<false><<<grid, 256, 0, s>>>(a);
+    LQ_LAUNCH_CHECK("gradient_sum_kernel");
+  }
+  return LQ_OK;
 }
 
 }  // namespace lq

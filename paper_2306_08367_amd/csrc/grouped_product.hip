@@ -280,6 +280,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
     for (int i = 0; i < B::PER; ++i) *reinterpret_cast<u32x4*>(to + A::BYTES + (i * THREADS + tid) * 16) = rb[i];
   };
 
+  const auto nothing = [](const u32x4(&)[S::NI]) {};
   for (;;) {
     f32x4 acc[S::MI][S::NI];
 #pragma unroll
@@ -288,14 +289,14 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
       for (int j = 0; j < S::NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (steps > 0) {
       if constexpr (DIRECT && THREADS == 512) {
-        multiply_in_turns<T, S, A, B>(lds, steps, issue, acc);
+        multiply_in_turns<T, S, A, B>(lds, steps, issue, acc, nothing);
       } else if constexpr (DIRECT) {
         issue(0, lds_address(lds));
         for (int step = 0; step < steps; ++step) {
           const int at = (step & 1) * BUFFER;
           meet_after_copies();     // this buffer is whole, the other one is read to its end
           if (step + 1 < steps) issue(step + 1, lds_address(lds) + (at ^ BUFFER));
-          multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc);
+          multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc, nothing);
         }
       } else {
         fetch(0);
@@ -304,7 +305,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
           const int at = (step & 1) * BUFFER;
           __syncthreads();         // likewise
           if (step + 1 < steps) fetch(step + 1);
-          multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc);
+          multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc, nothing);
           if (step + 1 < steps) put(lds + (at ^ BUFFER));
         }
       }
