@@ -156,41 +156,64 @@ template <int TM> __device__ __forceinline__ RowTile all_rows(int n, int id, int
   return tile_of_range<TM>(0, 0, n, die_order(id, (n + TM - 1) / TM * cols), cols);
 }
 
-// Rows of a group are added up in chunks of `most` rows.  Chunk `t`: group, rows, and among the chunks of the groups of more than
-// one the place of this chunk's partial sums (-1: the only chunk of its group).  A group without rows has one empty chunk.
-// group < 0: there is no such chunk.  Called by a whole wavefront, like find_tile.
+// Rows of a group are added up in chunks of about equal sizes, at most `most` rows each.
+__host__ __device__ inline int chunks_of(int rows, int most) { return rows > most ? (rows + most - 1) / most : 1; }
+__host__ __device__ inline int chunk_rows(int rows, int chunks) { return ((rows + chunks - 1) / chunks + 31) & ~31; }
+
+// Chunk number t: group, rows, and among the chunks of the groups of more than one the place of this chunk's partial sums (-1: the only
+// chunk of its group).  A group without rows has one empty chunk.  Up to 64 groups are taken by falling size of
+// their chunks, so that the long ones do not start last.  group < 0: there is no such chunk.  Called by a whole wavefront, like find_tile.
 struct Chunk { int group, first, rows, place; };
 __device__ __forceinline__ Chunk find_chunk(const int32_t* __restrict__ off, int G, int most, int t) {
   const int lane = threadIdx.x & 63;
   const int per = (G + 63) >> 6;
-  const int g0 = min(lane * per, G), g1 = min(g0 + per, G);
-  int own = 0, parts = 0;
+  int g0 = min(lane * per, G), g1 = min(g0 + per, G);
+  int own = 0, parts = 0, longest = 0;
   for (int g = g0; g < g1; ++g) {
-    const int c = max(1, (off[g + 1] - off[g] + most - 1) / most);
+    const int rows = off[g + 1] - off[g], c = chunks_of(rows, most);
     own += c;
     parts += c > 1 ? c : 0;
+    longest = chunk_rows(rows, c);
   }
-  int upto = own, parts_upto = parts;
+  int parts_upto = parts;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int v = __shfl_up(upto, d), w = __shfl_up(parts_upto, d);
-    if (lane >= d) {
-      upto += v;
-      parts_upto += w;
+    const int w = __shfl_up(parts_upto, d);
+    if (lane >= d) parts_upto += w;
+  }
+  int parts_before = parts_upto - parts;
+  if (per == 1) {
+    int rank = 0;
+    for (int g = 0; g < G; ++g) {
+      const int other = __builtin_amdgcn_readlane(longest, g);
+      rank += other > longest || (other == longest && g < lane);
     }
+    if (lane >= G) rank = lane;
+    const int from = __builtin_amdgcn_ds_permute(rank * 4, lane);     // the group of this rank
+    own = __shfl(own, from);
+    parts_before = __shfl(parts_before, from);
+    g0 = from < G ? from : G;
+    g1 = from < G ? from + 1 : G;
+  }
+  int upto = own;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(upto, d);
+    if (lane >= d) upto += v;
   }
   const unsigned long long holds = __ballot(upto > t);
   if (!holds) return {-1, 0, 0, -1};
   const int at = __ffsll(static_cast<long long>(holds)) - 1;
   int group = 0, first = 0, rows = 0, place = -1;
   if (lane == at) {
-    int before = upto - own, parts_before = parts_upto - parts;
+    int before = upto - own;
     for (int g = g0; g < g1; ++g) {
-      const int b = off[g], e = off[g + 1], c = max(1, (e - b + most - 1) / most);
+      const int b = off[g], e = off[g + 1], c = chunks_of(e - b, most);
       if (t < before + c) {
+        const int step = chunk_rows(e - b, c);
         group = g;
-        first = b + (t - before) * most;
-        rows = min(most, e - first);
+        first = min(b + (t - before) * step, e);
+        rows = min(step, e - first);
         place = c > 1 ? parts_before + t - before : -1;
         break;
       }

@@ -28,7 +28,8 @@ template <bool BF16> __device__ __forceinline__ void store_values(void* base, in
     }
 }
 
-constexpr int SEGMENT = 4096;     // rows whose numbers are held in LDS at a time
+constexpr int SEGMENT = 2048;     // rows whose numbers are held in LDS at a time
+constexpr int RUN = 32;           // most tiles of a chunk that go to one die together
 
 template <typename T, class S, bool DIRECT>
 __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(GradientArgs a) {
@@ -37,13 +38,17 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(Gradien
   typedef Operand<T, false, S::TN, S::THREADS, KBYTES> B;
   constexpr int KSTEP = A::KSTEP, EPC = A::EPC, THREADS = S::THREADS, BUFFER = A::BYTES + B::BYTES;
   extern __shared__ __align__(1024) char lds[];
-  __shared__ int row[SEGMENT];
+  __shared__ int xrow[SEGMENT], yrow[SEGMENT];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int tiles = a.tiles_m * a.tiles_n;
-  const int id = die_order(blockIdx.x, gridDim.x);
-  const Chunk chunk = find_chunk(a.off, a.G, a.most, id / tiles);
+  // Workgroups go to the 8 dies in turn.  The tiles of a chunk, which share its rows, go to one die in runs of up to 32 (a
+  // die's compute units), the runs to the dies forth and back, so that each gets long and short ones.
+  const int tiles = a.tiles_m * a.tiles_n, run_tiles = min(tiles, RUN), runs = (tiles + run_tiles - 1) / run_tiles;
+  const int die = blockIdx.x & 7, turn = (blockIdx.x >> 3) / run_tiles;
+  const int run = turn * 8 + ((turn & 1) ? 7 - die : die), tile = run % runs * run_tiles + (blockIdx.x >> 3) % run_tiles;
+  if (tile >= tiles) return;
+  const Chunk chunk = find_chunk(a.off, a.G, a.most, run / runs);
   if (chunk.group < 0) return;
-  const int tm = id % tiles / a.tiles_n, tn = id % tiles % a.tiles_n;
+  const int tm = tile / a.tiles_n, tn = tile % a.tiles_n;
   const int m0 = tm * S::TM, n0 = tn * S::TN;
 
   f32x4 acc[S::MI][S::NI], sum[S::NI];
@@ -74,27 +79,43 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(Gradien
   for (int s0 = 0; s0 < chunk.rows; s0 += SEGMENT) {
     const int first = chunk.first + s0, rows = min(SEGMENT, chunk.rows - s0), steps = (rows + KSTEP - 1) / KSTEP;
     __syncthreads();     // (the segment before is read to its end)
-    for (int i = tid; i < rows; i += THREADS) row[i] = a.order ? a.order[first + i] : first + i;
+    for (int i = tid; i < rows; i += THREADS) {
+      const int p = first + i, r = a.order ? a.order[p] : p;
+      xrow[i] = a.x_grouped ? p : r / a.slots;
+      yrow[i] = a.y_grouped ? p : r;
+    }
     __syncthreads();
-    auto x_row = [&](int line) { return X + static_cast<int64_t>(a.x_grouped ? first + line : row[line] / a.slots) * a.ldx; };
-    auto y_row = [&](int line) { return dY + static_cast<int64_t>(a.y_grouped ? first + line : row[line]) * a.ldy; };
-    auto issue = [&](int step, unsigned int to) {
-      const int k0 = step * KSTEP;
-      to += wave * 1024;
-      // (rows behind the last one are zeros in both operands)
+    auto x_row = [&](int line) { return X + xrow[line] * a.ldx; };
+    auto y_row = [&](int line) { return dY + yrow[line] * a.ldy; };
+    // Where the pieces of a step lie (rows behind the last one: zeros in both operands), worked out ahead of their copies.
+    const void *pa[A::PER], *pb[B::PER];
+    int ready = -1;
+    auto prepare = [&](int step) {
 #pragma unroll
       for (int i = 0; i < A::PER; ++i) {
-        const int line = k0 + A::line_of(i);
-        copy_to_lds(line < rows ? static_cast<const void*>(x_row(line) + ca[i]) : &g_zeros, to + i * THREADS * 16);
+        const int line = step * KSTEP + A::line_of(i);
+        pa[i] = line < rows ? static_cast<const void*>(x_row(line) + ca[i]) : &g_zeros;
       }
 #pragma unroll
       for (int i = 0; i < B::PER; ++i) {
-        const int line = k0 + B::line_of(i);
-        copy_to_lds(line < rows ? static_cast<const void*>(y_row(line) + cb[i]) : &g_zeros, to + A::BYTES + i * THREADS * 16);
+        const int line = step * KSTEP + B::line_of(i);
+        pb[i] = line < rows ? static_cast<const void*>(y_row(line) + cb[i]) : &g_zeros;
       }
+      ready = step;
+    };
+    auto issue = [&](int step, unsigned int to) {
+      if (ready != step) prepare(step);
+      to += wave * 1024;
+#pragma unroll
+      for (int i = 0; i < A::PER; ++i) copy_to_lds(pa[i], to + i * THREADS * 16);
+#pragma unroll
+      for (int i = 0; i < B::PER; ++i) copy_to_lds(pb[i], to + A::BYTES + i * THREADS * 16);
     };
     if constexpr (DIRECT && THREADS == 512) {
-      multiply_in_turns<T, S, A, B>(lds, steps, issue, acc, add_up);
+      multiply_in_turns<T, S, A, B>(lds, steps, issue, acc, [&](const u32x4(&b)[S::NI]) {
+        add_up(b);
+        prepare(ready + 1);
+      });
     } else if constexpr (DIRECT) {
       issue(0, lds_address(lds));
       for (int step = 0; step < steps; ++step) {
@@ -165,7 +186,7 @@ template <bool BF16> __global__ __launch_bounds__(256) void gradient_sum_kernel(
   const int per = (a.G + 63) >> 6, g0 = min(lane * per, a.G), g1 = min(g0 + per, a.G);
   int own = 0, parts = 0;
   for (int g = g0; g < g1; ++g) {
-    const int c = (a.off[g + 1] - a.off[g] + a.most - 1) / a.most;
+    const int c = chunks_of(a.off[g + 1] - a.off[g], a.most);
     own += c > 1;
     parts += c > 1 ? c : 0;
   }
@@ -187,7 +208,7 @@ template <bool BF16> __global__ __launch_bounds__(256) void gradient_sum_kernel(
     int left = which - (upto - own);
     first = parts_upto - parts;
     for (int g = g0; g < g1; ++g) {
-      const int c = (a.off[g + 1] - a.off[g] + a.most - 1) / a.most;
+      const int c = chunks_of(a.off[g + 1] - a.off[g], a.most);
       if (c <= 1) continue;
       if (left-- == 0) {
         group = g;
@@ -244,8 +265,9 @@ template <typename T, class S, bool DIRECT> int launch(GradientArgs a, const Pla
   constexpr int LDS = (S::THREADS == 512 ? 4 : 2) * (A::BYTES + B::BYTES);
   a.tiles_m = (a.k + S::TM - 1) / S::TM;
   a.tiles_n = (a.l + S::TN - 1) / S::TN;
-  const int64_t chunks = a.n / p.most + a.G;
-  const int64_t blocks = chunks * a.tiles_m * a.tiles_n;
+  const int64_t chunks = a.n / p.most + a.G, tiles = static_cast<int64_t>(a.tiles_m) * a.tiles_n;
+  const int64_t run_tiles = std::min<int64_t>(tiles, RUN), runs = chunks * ((tiles + run_tiles - 1) / run_tiles);
+  const int64_t blocks = (runs + 7) / 8 * 8 * run_tiles;
   if (blocks > 0x7fffffff) return fail(LQ_ERR_UNSUPPORTED, "grouped gradient: %lld tiles are more than one launch takes", (long long)blocks);
   const auto kernel = grouped_gradient_kernel<T, S, DIRECT>;
   if (LDS + SEGMENT * 4 > 48 * 1024)
