@@ -207,7 +207,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
   }
   const int64_t step_b = BT ? 1 : a.ldw;     // elements per inner index
   constexpr int BUFFER = A::BYTES + B::BYTES, SLOTS = KSTEP / EPC;
-  const int own_steps = any ? (k_end - k_first + KSTEP - 1) / KSTEP : 0;
+  const int own_steps = __builtin_amdgcn_readfirstlane(any ? (k_end - k_first + KSTEP - 1) / KSTEP : 0);
   // The adapters' steps: pieces of EPC inner indexes, two for every 8 ranks of every adapter: bf16: U's leading part and the
   // rest of it, times the same ranks of B; fp32: the two halves of the 8.
   const int per = ADAPT ? a.rp >> 3 : 1;
