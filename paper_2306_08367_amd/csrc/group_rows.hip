@@ -5,7 +5,9 @@
 //   first place of the group + rows of earlier workgroups + of earlier wavefronts + of earlier lanes with the same key,
 // where the last term comes from comparing the 64 keys of a step bit by bit (ballots): no atomic decides a place, so the
 // order is the rows' own.  Few keys are done by one workgroup in one launch; more take three launches: counts per
-// workgroup, sums of those over the workgroups, places.
+// workgroup, sums of those over the workgroups, places.  There a workgroup first sorts 8,192 rows in LDS and then writes them out
+// in that order, so that neighbouring lanes write neighbouring places (6e6 keys in 2,000 groups, scattered one by
+// one: 74 us; so: see place_sorted), as long as LDS holds that beside the counts.
 // A key outside [0, G) counts as group G, whose rows come last.
 #include "grouped.h"
 
@@ -62,10 +64,18 @@ __device__ __forceinline__ void wave_run(int64_t begin, int64_t end, int64_t* b,
   *e = min(*b + per, end);
 }
 
+constexpr int AHEAD = 8;      // keys of a lane whose loads are under way together
+
 __device__ __forceinline__ void count_keys(const int32_t* __restrict__ keys, int G, int64_t b, int64_t e, unsigned int* mine) {
-  for (int64_t i = b + (threadIdx.x & 63); i < e; i += 64) {
-    const int g = group_of_key(keys[i], G);
-    atomicAdd(&mine[g >> 1], 1u << (16 * (g & 1)));
+  for (int64_t i0 = b + (threadIdx.x & 63); i0 < e; i0 += 64 * AHEAD) {
+    int key[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) key[j] = i0 + 64 * j < e ? keys[i0 + 64 * j] : 0;
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int g = group_of_key(key[j], G);
+      if (i0 + 64 * j < e) atomicAdd(&mine[g >> 1], 1u << (16 * (g & 1)));
+    }
   }
 }
 
@@ -84,21 +94,31 @@ template <typename F> __device__ __forceinline__ void sum_waves(int G, unsigned 
   }
 }
 
+// put(row, group, place) for the rows of the wavefront's run, in their order; base: first places of the groups.
+template <typename F>
 __device__ __forceinline__ void place_rows(const int32_t* __restrict__ keys, int G, int bits, int64_t b, int64_t e, const int* base,
-                                           unsigned short* mine, int32_t* __restrict__ order) {
+                                           unsigned short* mine, F&& put) {
   const int lane = threadIdx.x & 63;
-  for (int64_t i0 = b; i0 < e; i0 += 64) {
-    const int64_t i = i0 + lane;
-    const bool in = i < e;
-    const int g = in ? group_of_key(keys[i], G) : 0;
-    const unsigned long long same = same_key(g, bits, __ballot(in));
-    if (in) {
-      const int earlier = __popcll(same & ((1ull << lane) - 1));
-      const int before = mine[g];
-      order[base[g] + before + earlier] = static_cast<int32_t>(i);
-      if (earlier == 0) mine[g] = static_cast<unsigned short>(before + __popcll(same));
+  for (int64_t i0 = b; i0 < e; i0 += 64 * AHEAD) {
+    int key[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) key[j] = i0 + 64 * j + lane < e ? keys[i0 + 64 * j + lane] : 0;
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int64_t i = i0 + 64 * j + lane;
+      const bool in = i < e;
+      const unsigned long long some = __ballot(in);
+      if (!some) break;
+      const int g = group_of_key(key[j], G);
+      const unsigned long long same = same_key(g, bits, some);
+      if (in) {
+        const int earlier = __popcll(same & ((1ull << lane) - 1));
+        const int before = mine[g];
+        put(i, g, base[g] + before + earlier);
+        if (earlier == 0) mine[g] = static_cast<unsigned short>(before + __popcll(same));
+      }
+      __builtin_amdgcn_wave_barrier();     // (the next step's lanes read what this one's wrote: LDS keeps a wavefront's order)
     }
-    __builtin_amdgcn_wave_barrier();     // (the next step's lanes read what this one's wrote: LDS keeps a wavefront's order)
   }
 }
 
@@ -129,7 +149,8 @@ __global__ __launch_bounds__(THREADS) void group_rows_kernel(const int32_t* __re
     first += total;
   }
   __syncthreads();
-  place_rows(keys, G, bits, b, e, shared_base, reinterpret_cast<unsigned short*>(mine), order);
+  place_rows(keys, G, bits, b, e, shared_base, reinterpret_cast<unsigned short*>(mine),
+             [&](int64_t row, int, int place) { order[place] = static_cast<int32_t>(row); });
 }
 
 __global__ __launch_bounds__(THREADS) void group_count_kernel(const int32_t* __restrict__ keys, int64_t n, int64_t per, int G,
@@ -138,74 +159,118 @@ __global__ __launch_bounds__(THREADS) void group_count_kernel(const int32_t* __r
   for (int g = threadIdx.x; g <= G; g += THREADS) hist[g] = 0;
   __syncthreads();
   const int64_t begin = blockIdx.x * per, end = min(begin + per, n);
-  for (int64_t i = begin + threadIdx.x; i < end; i += THREADS) atomicAdd(&hist[group_of_key(keys[i], G)], 1);
+  for (int64_t i0 = begin + threadIdx.x; i0 < end; i0 += THREADS * AHEAD) {
+    int key[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) key[j] = i0 + j * THREADS < end ? keys[i0 + j * THREADS] : 0;
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+      if (i0 + j * THREADS < end) atomicAdd(&hist[group_of_key(key[j], G)], 1);
+  }
   __syncthreads();
   for (int g = threadIdx.x; g <= G; g += THREADS) counts[static_cast<int64_t>(blockIdx.x) * (G + 1) + g] = hist[g];
 }
 
-// counts[b][g] becomes the rows of group g in workgroups before b; totals[g] all of them.  64 groups a workgroup, the
-// workgroups' counts in 16 parts.
+// counts[b][g] becomes the rows of group g in workgroups before b; totals[g] all of them.  16 groups a workgroup, the
+// workgroups' counts in 64 parts.
+constexpr int SUM_GROUPS = 16, SUM_PARTS = THREADS / SUM_GROUPS;
 __global__ __launch_bounds__(THREADS) void group_sum_kernel(int blocks, int G, int32_t* __restrict__ counts, int32_t* __restrict__ totals) {
-  __shared__ int part[WAVES][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = blockIdx.x * 64 + lane;
-  const int per = (blocks + WAVES - 1) / WAVES, b0 = min(wave * per, blocks), b1 = min(b0 + per, blocks);
+  __shared__ int part[SUM_PARTS][SUM_GROUPS];
+  const int lane = threadIdx.x % SUM_GROUPS, p = threadIdx.x / SUM_GROUPS, g = blockIdx.x * SUM_GROUPS + lane;
+  const int per = (blocks + SUM_PARTS - 1) / SUM_PARTS, b0 = min(p * per, blocks), b1 = min(b0 + per, blocks);
   int sum = 0;
   if (g <= G)
     for (int b = b0; b < b1; ++b) sum += counts[static_cast<int64_t>(b) * (G + 1) + g];
-  part[wave][lane] = sum;
+  part[p][lane] = sum;
   __syncthreads();
-  int before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    before += w < wave ? part[w][lane] : 0;
-    all += part[w][lane];
-  }
+  int before = 0;
+  for (int w = 0; w < p; ++w) before += part[w][lane];
   if (g > G) return;
+  if (p == SUM_PARTS - 1) totals[g] = before + sum;
   for (int b = b0; b < b1; ++b) {
     const int64_t at = static_cast<int64_t>(b) * (G + 1) + g;
     const int v = counts[at];
     counts[at] = before;
     before += v;
   }
-  if (wave == 0) totals[g] = all;
 }
 
+// LDS of the sorting form: next places [G + 1], counts per wavefront, and of SORTED rows at a time their numbers and groups in sorted
+// order and the groups' first places among them.
+constexpr int SORTED = THREADS * AHEAD;
+inline size_t sorted_lds(int G) { return place_lds(G) + (static_cast<size_t>(G) + 1) * 4 + SORTED * 4; }
+
+template <bool SORT>
 __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __restrict__ keys, int64_t n, int64_t per, int G, int bits,
                                                               const int32_t* __restrict__ counts, const int32_t* __restrict__ totals,
                                                               int32_t* __restrict__ off, int32_t* __restrict__ order) {
-  extern __shared__ int shared_base[];
+  extern __shared__ int next[];         // where a group's next row goes
   __shared__ int waves[WAVES];
-  unsigned int* own = reinterpret_cast<unsigned int*>(shared_base + G + 1);
   const int words = count_words(G);
-  for (int i = threadIdx.x; i < WAVES * words; i += THREADS) own[i] = 0;
-  __syncthreads();
-  const int64_t begin = blockIdx.x * per, end = min(begin + per, n);
-  int64_t b, e;
-  wave_run(begin, max(begin, end), &b, &e);
+  unsigned int* own = reinterpret_cast<unsigned int*>(next + G + 1);
+  unsigned short* own16 = reinterpret_cast<unsigned short*>(own);
   unsigned int* mine = own + (threadIdx.x >> 6) * words;
-  count_keys(keys, G, b, e, mine);
+  int* local = reinterpret_cast<int*>(own + WAVES * words);                       // SORT: first place of a group among the SORTED rows
+  unsigned short* row = reinterpret_cast<unsigned short*>(local + G + 1);         // SORT: [SORTED] row - first row of them
+  unsigned short* group = row + SORTED;                                           // SORT: [SORTED]
+  const int64_t begin = blockIdx.x * per, end = min(begin + per, n);
   int first = 0;
   for (int g0 = 0; g0 <= G; g0 += THREADS) {
     const int g = g0 + threadIdx.x;
     int total;
     const int before = scan_threads(g <= G ? totals[g] : 0, waves, &total);
     if (g <= G) {
-      shared_base[g] = first + before + counts[static_cast<int64_t>(blockIdx.x) * (G + 1) + g];
+      next[g] = first + before + counts[static_cast<int64_t>(blockIdx.x) * (G + 1) + g];
       if (blockIdx.x == 0) off[g] = first + before;
     }
     first += total;
   }
-  __syncthreads();
-  sum_waves(G, reinterpret_cast<unsigned short*>(own), [](int, int) {});
-  __syncthreads();
-  place_rows(keys, G, bits, b, e, shared_base, reinterpret_cast<unsigned short*>(mine), order);
+  for (int64_t at = begin; at < end; at += SORT ? SORTED : per) {
+    const int64_t to = SORT ? min(at + SORTED, end) : end;
+    for (int i = threadIdx.x; i < WAVES * words; i += THREADS) own[i] = 0;
+    __syncthreads();
+    int64_t b, e;
+    wave_run(at, to, &b, &e);
+    count_keys(keys, G, b, e, mine);
+    __syncthreads();
+    if constexpr (SORT) {
+      sum_waves(G, own16, [&](int g, int sum) { local[g] = sum; });
+      __syncthreads();
+      int before_all = 0;
+      for (int g0 = 0; g0 <= G; g0 += THREADS) {
+        const int g = g0 + threadIdx.x;
+        int total;
+        const int before = scan_threads(g <= G ? local[g] : 0, waves, &total);
+        if (g <= G) local[g] = before_all + before;
+        before_all += total;
+      }
+      __syncthreads();
+      place_rows(keys, G, bits, b, e, local, reinterpret_cast<unsigned short*>(mine), [&](int64_t r, int g, int place) {
+        row[place] = static_cast<unsigned short>(r - at);
+        group[place] = static_cast<unsigned short>(g);
+      });
+      __syncthreads();
+      const int here = static_cast<int>(to - at);
+      for (int i = threadIdx.x; i < here; i += THREADS) {
+        const int g = group[i];
+        order[next[g] + i - local[g]] = static_cast<int32_t>(at) + row[i];
+      }
+      __syncthreads();
+      for (int g = threadIdx.x; g <= G; g += THREADS) next[g] += (g < G ? local[g + 1] : here) - local[g];
+    } else {
+      sum_waves(G, own16, [](int, int) {});
+      __syncthreads();
+      place_rows(keys, G, bits, b, e, next, reinterpret_cast<unsigned short*>(mine),
+                 [&](int64_t r, int, int place) { order[place] = static_cast<int32_t>(r); });
+    }
+  }
 }
 
 // Keys and number of workgroups of the three-launch form: 256 workgroups (one a compute unit) unless that leaves them fewer
-// than 4,096 keys, and at most 512K keys each (16-bit counts per wavefront hold 65,535).
+// than 8,192 keys, and at most 512K keys each (16-bit counts per wavefront hold 65,535).
 void split(int64_t n, int64_t* per, int* blocks) {
-  int64_t p = std::max<int64_t>(4096, (n + 255) / 256);
-  p = std::min<int64_t>((p + 1023) / 1024 * 1024, 1 << 19);
+  int64_t p = std::max<int64_t>(SORTED, (n + 255) / 256);
+  p = std::min<int64_t>((p + SORTED - 1) / SORTED * SORTED, 1 << 19);
   *per = p;
   *blocks = static_cast<int>((n + p - 1) / p);
 }
@@ -262,12 +327,14 @@ int launch_group_rows(const int32_t* keys, int64_t n, int32_t G, int32_t* off, i
   int32_t* totals = counts + static_cast<int64_t>(blocks) * (G + 1);
   group_count_kernel<<<blocks, THREADS, (G + 1) * 4, s>>>(keys, n, per, G, counts);
   LQ_LAUNCH_CHECK("group_count_kernel");
-  group_sum_kernel<<<(G + 64) / 64, THREADS, 0, s>>>(blocks, G, counts, totals);
+  group_sum_kernel<<<G / SUM_GROUPS + 1, THREADS, 0, s>>>(blocks, G, counts, totals);
   LQ_LAUNCH_CHECK("group_sum_kernel");
-  if (lds > 64 * 1024)
-    LQ_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&group_place_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                   static_cast<int>(lds)));
-  group_place_kernel<<<blocks, THREADS, lds, s>>>(keys, n, per, G, bits, counts, totals, off, order);
+  const bool sort = sorted_lds(G) <= 156 * 1024;
+  const size_t bytes = sort ? sorted_lds(G) : lds;
+  const auto kernel = sort ? group_place_kernel<true> : group_place_kernel<false>;
+  if (bytes > 64 * 1024)
+    LQ_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+  kernel<<<blocks, THREADS, bytes, s>>>(keys, n, per, G, bits, counts, totals, off, order);
   LQ_LAUNCH_CHECK("group_place_kernel");
   return LQ_OK;
 }

@@ -385,11 +385,11 @@ __device__ __forceinline__ void multiply_in_turns(char* lds, int units, F&& issu
     if (second) wait_copies(u + 3 < units);
     turn();
     __builtin_amdgcn_s_setprio(1);
+    with_b(b);
 #pragma unroll
     for (int i = 0; i < S::MI; ++i)
 #pragma unroll
       for (int j = 0; j < S::NI; ++j) acc[i][j] = multiply<T>(b[j], a[i], acc[i][j]);
-    with_b(b);
     __builtin_amdgcn_s_setprio(0);
     if (!second) wait_copies(u + 3 < units);
     turn();

@@ -87,34 +87,41 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(Gradien
     __syncthreads();
     auto x_row = [&](int line) { return X + xrow[line] * a.ldx; };
     auto y_row = [&](int line) { return dY + yrow[line] * a.ldy; };
-    // Where the pieces of a step lie (rows behind the last one: zeros in both operands), worked out ahead of their copies.
-    const void *pa[A::PER], *pb[B::PER];
-    int ready = -1;
-    auto prepare = [&](int step) {
+    // Where the pieces of a step lie (rows behind the last one: zeros in both operands).  Row numbers are read from LDS together
+    // with operands and made addresses beside the products, a block ahead of their copies.
+    constexpr int COPIES = A::PER + B::PER;
+    const void* from[COPIES];
+    int number[COPIES], ready = -1, looked = -1;
+    auto look_up = [&](int step) {
 #pragma unroll
-      for (int i = 0; i < A::PER; ++i) {
-        const int line = step * KSTEP + A::line_of(i);
-        pa[i] = line < rows ? static_cast<const void*>(x_row(line) + ca[i]) : &g_zeros;
+      for (int c = 0; c < COPIES; ++c) {
+        const int line = step * KSTEP + (c >= A::PER ? B::line_of(c - A::PER) : A::line_of(c));
+        number[c] = line < rows ? (c >= A::PER ? yrow[line] : xrow[line]) : -1;
       }
+      looked = step;
+    };
+    auto locate = [&]() {
 #pragma unroll
-      for (int i = 0; i < B::PER; ++i) {
-        const int line = step * KSTEP + B::line_of(i);
-        pb[i] = line < rows ? static_cast<const void*>(y_row(line) + cb[i]) : &g_zeros;
+      for (int c = 0; c < COPIES; ++c) {
+        const T* p = c >= A::PER ? dY + number[c] * a.ldy + cb[c - A::PER] : X + number[c] * a.ldx + ca[c];
+        from[c] = number[c] >= 0 ? static_cast<const void*>(p) : &g_zeros;
       }
-      ready = step;
+      ready = looked;
     };
     auto issue = [&](int step, unsigned int to) {
-      if (ready != step) prepare(step);
-      to += wave * 1024;
+      if (ready != step) {
+        look_up(step);
+        locate();
+      }
 #pragma unroll
-      for (int i = 0; i < A::PER; ++i) copy_to_lds(pa[i], to + i * THREADS * 16);
-#pragma unroll
-      for (int i = 0; i < B::PER; ++i) copy_to_lds(pb[i], to + A::BYTES + i * THREADS * 16);
+      for (int c = 0; c < COPIES; ++c)
+        copy_to_lds(from[c], to + wave * 1024 + (c >= A::PER ? A::BYTES + (c - A::PER) * THREADS * 16 : c * THREADS * 16));
+      look_up(step + 1);
     };
     if constexpr (DIRECT && THREADS == 512) {
       multiply_in_turns<T, S, A, B>(lds, steps, issue, acc, [&](const u32x4(&b)[S::NI]) {
         add_up(b);
-        prepare(ready + 1);
+        locate();
       });
     } else if constexpr (DIRECT) {
       issue(0, lds_address(lds));
