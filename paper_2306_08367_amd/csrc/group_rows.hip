@@ -3,8 +3,8 @@
 // A workgroup takes a run of keys and each of its wavefronts a run of that.  Two passes over the keys: the first counts
 // the keys of every group per wavefront (LDS), the second puts every row at
 //   first place of the group + rows of earlier workgroups + of earlier wavefronts + of earlier lanes with the same key,
-// where the last term comes from comparing the 64 keys of a step bit by bit (ballots): no atomic decides a place, so the
-// order is the rows' own.  Few keys are done by one workgroup in one launch; more take three launches: counts per
+// where the last term comes from comparing the keys of a step that share a group with another one (ballots): no atomic decides a
+// place, so the order is the rows' own.  Few keys are done by one workgroup in one launch; more take three launches: counts per
 // workgroup, sums of those over the workgroups, places.  There a workgroup first sorts 8,192 rows in LDS and then writes them out
 // in that order, so that neighbouring lanes write neighbouring places (6e6 keys in 2,000 groups, scattered one by
 // one: 74 us; so: see place_sorted), as long as LDS holds that beside the counts.
@@ -19,15 +19,28 @@ constexpr int64_t ONE_GROUP_KEYS = 16384;    // most keys of the one-workgroup f
 
 __device__ __forceinline__ int group_of_key(int key, int G) { return static_cast<unsigned>(key) < static_cast<unsigned>(G) ? key : G; }
 
-// Lanes of the wavefront whose key equals this lane's, among those of `active`.
-__device__ __forceinline__ unsigned long long same_key(int key, int bits, unsigned long long active) {
-  unsigned long long m = active;
-  for (int b = 0; b < bits; ++b) {
-    const bool one = (key >> b) & 1;
-    const unsigned long long v = __ballot(one);
-    m &= one ? v : ~v;
+// How many lanes below this one hold the same group, of those of `active`; `shared`: whether this lane's group is another active
+// lane's as well.  A few such groups are gone through one by one; from many on, all lanes are compared bit by bit.
+__device__ __forceinline__ int lanes_before(int g, int bits, bool shared, unsigned long long active) {
+  const unsigned long long below = (1ull << (threadIdx.x & 63)) - 1;
+  unsigned long long left = __ballot(shared);
+  int before = 0;
+  if (__popcll(left) <= 24) {
+    while (left) {
+      const int leader = __builtin_amdgcn_readlane(g, __ffsll(static_cast<long long>(left)) - 1);
+      const unsigned long long same = __ballot(g == leader) & left;
+      if (g == leader) before = __popcll(same & below);
+      left &= ~same;
+    }
+    return before;
   }
-  return m;
+  unsigned long long same = active;
+  for (int b = 0; b < bits; ++b) {
+    const bool one = (g >> b) & 1;
+    const unsigned long long v = __ballot(one);
+    same &= one ? v : ~v;
+  }
+  return __popcll(same & below);
 }
 
 // Sum over the workgroup's threads below this one; *total: over all.
@@ -83,12 +96,13 @@ __device__ __forceinline__ void count_keys(const int32_t* __restrict__ keys, int
 template <typename F> __device__ __forceinline__ void sum_waves(int G, unsigned short* counts, F&& total) {
   const int stride = 2 * count_words(G);
   for (int g = threadIdx.x; g <= G; g += THREADS) {
-    int sum = 0;
+    int v[WAVES], sum = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v[w] = counts[w * stride + g];
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-      const int v = counts[w * stride + g];
       counts[w * stride + g] = static_cast<unsigned short>(sum);
-      sum += v;
+      sum += v[w];
     }
     total(g, sum);
   }
@@ -97,8 +111,9 @@ template <typename F> __device__ __forceinline__ void sum_waves(int G, unsigned 
 // put(row, group, place) for the rows of the wavefront's run, in their order; base: first places of the groups.
 template <typename F>
 __device__ __forceinline__ void place_rows(const int32_t* __restrict__ keys, int G, int bits, int64_t b, int64_t e, const int* base,
-                                           unsigned short* mine, F&& put) {
+                                           unsigned int* mine, F&& put) {
   const int lane = threadIdx.x & 63;
+  const volatile unsigned short* mine16 = reinterpret_cast<unsigned short*>(mine);
   for (int64_t i0 = b; i0 < e; i0 += 64 * AHEAD) {
     int key[AHEAD];
 #pragma unroll
@@ -109,15 +124,17 @@ __device__ __forceinline__ void place_rows(const int32_t* __restrict__ keys, int
       const bool in = i < e;
       const unsigned long long some = __ballot(in);
       if (!some) break;
-      const int g = group_of_key(key[j], G);
-      const unsigned long long same = same_key(g, bits, some);
-      if (in) {
-        const int earlier = __popcll(same & ((1ull << lane) - 1));
-        const int before = mine[g];
-        put(i, g, base[g] + before + earlier);
-        if (earlier == 0) mine[g] = static_cast<unsigned short>(before + __popcll(same));
-      }
-      __builtin_amdgcn_wave_barrier();     // (the next step's lanes read what this one's wrote: LDS keeps a wavefront's order)
+      const int g = in ? group_of_key(key[j], G) : -1;
+      // (LDS keeps a wavefront's order: the counts before this step, with this step's rows, and then read again)
+      int earlier = 0, after = 0;
+      if (in) earlier = mine16[g];
+      __builtin_amdgcn_wave_barrier();
+      if (in) atomicAdd(&mine[g >> 1], 1u << (16 * (g & 1)));
+      __builtin_amdgcn_wave_barrier();
+      if (in) after = mine16[g];
+      const int before = lanes_before(g, bits, in && after - earlier > 1, some);
+      if (in) put(i, g, base[g] + earlier + before);
+      __builtin_amdgcn_wave_barrier();
     }
   }
 }
@@ -149,7 +166,7 @@ __global__ __launch_bounds__(THREADS) void group_rows_kernel(const int32_t* __re
     first += total;
   }
   __syncthreads();
-  place_rows(keys, G, bits, b, e, shared_base, reinterpret_cast<unsigned short*>(mine),
+  place_rows(keys, G, bits, b, e, shared_base, mine,
              [&](int64_t row, int, int place) { order[place] = static_cast<int32_t>(row); });
 }
 
@@ -245,7 +262,7 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
         before_all += total;
       }
       __syncthreads();
-      place_rows(keys, G, bits, b, e, local, reinterpret_cast<unsigned short*>(mine), [&](int64_t r, int g, int place) {
+      place_rows(keys, G, bits, b, e, local, mine, [&](int64_t r, int g, int place) {
         row[place] = static_cast<unsigned short>(r - at);
         group[place] = static_cast<unsigned short>(g);
       });
@@ -260,7 +277,7 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
     } else {
       sum_waves(G, own16, [](int, int) {});
       __syncthreads();
-      place_rows(keys, G, bits, b, e, next, reinterpret_cast<unsigned short*>(mine),
+      place_rows(keys, G, bits, b, e, next, mine,
                  [&](int64_t r, int, int place) { order[place] = static_cast<int32_t>(r); });
     }
   }
