@@ -22,7 +22,7 @@ struct GroupedArgs {
   int32_t slots;          // row r of Y reads row r / slots of X
   int32_t x_grouped, y_grouped;
   int32_t relu, y_bf16;
-  int32_t y_vec;          // four results of a row may be loaded and stored together
+  int32_t y_vec;          // rows of Y, bias and gate are aligned to 16 bytes
   int32_t tiles_n, row_tiles;
   int32_t steps_per_split;   // K steps of one split; split z writes at Y + z * split_stride
   int64_t split_stride;
@@ -39,7 +39,7 @@ struct GradientArgs {
   int32_t G, n;
   const void* X; int64_t ldx; int32_t slots, x_grouped;
   const void* dY; int64_t ldy; int32_t y_grouped;
-  void* dW; int64_t ldw, sw; int32_t w_bf16, w_vec;
+  void* dW; int64_t ldw, sw; int32_t w_bf16;
   void* db; int64_t ldb;
   int32_t k, l;
   int32_t tiles_m, tiles_n;
@@ -71,13 +71,18 @@ static __device__ const u32x4 g_zeros = {0, 0, 0, 0};
 
 struct __attribute__((packed, aligned(2))) Bytes16 { unsigned int x, y, z, w; };
 
-// The 16 bytes at p, of which only the first `valid` elements exist (the others read as zero); any alignment.
+struct __attribute__((packed, aligned(2))) Bytes8 { unsigned int x, y; };
+
+// The 16 bytes at p, any alignment.
+template <typename T> __device__ __forceinline__ u32x4 load_whole(const T* p) {
+  const Bytes16 t = *reinterpret_cast<const Bytes16*>(p);
+  return u32x4{t.x, t.y, t.z, t.w};
+}
+
+// The same where only the first `valid` elements exist (the others read as zero).
 template <typename T> __device__ __forceinline__ u32x4 load_piece(const T* p, int valid) {
   constexpr int PER = 16 / sizeof(T);
-  if (valid >= PER) {
-    const Bytes16 t = *reinterpret_cast<const Bytes16*>(p);
-    return u32x4{t.x, t.y, t.z, t.w};
-  }
+  if (valid >= PER) return load_whole(p);
   u32x4 r = {0, 0, 0, 0};
 #pragma unroll
   for (int q = 0; q < PER; ++q)
@@ -85,6 +90,49 @@ template <typename T> __device__ __forceinline__ u32x4 load_piece(const T* p, in
       if constexpr (sizeof(T) == 4) r[q] = reinterpret_cast<const unsigned int*>(p)[q];
       else r[q >> 1] |= static_cast<unsigned int>(p[q]) << (16 * (q & 1));
     }
+  return r;
+}
+
+// Four neighbouring results at p, of which the first `valid` exist; any alignment.
+template <bool BF16> __device__ __forceinline__ void store_four(void* base, int64_t at, int valid, f32x4 v) {
+  if constexpr (BF16) {
+    bf16_t* p = static_cast<bf16_t*>(base) + at;
+    const unsigned int lo = f32x2_to_bf16x2(v[0], v[1]), hi = f32x2_to_bf16x2(v[2], v[3]);
+    if (valid >= 4) {
+      *reinterpret_cast<Bytes8*>(p) = Bytes8{lo, hi};
+      return;
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
+      if (q < valid) p[q] = static_cast<bf16_t>((q < 2 ? lo : hi) >> (16 * (q & 1)));
+  } else {
+    float* p = static_cast<float*>(base) + at;
+    if (valid >= 4) {
+      *reinterpret_cast<Bytes16*>(p) = Bytes16{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+      return;
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
+      if (q < valid) p[q] = v[q];
+  }
+}
+
+// Four neighbouring values at p, likewise.
+template <typename T> __device__ __forceinline__ f32x4 load_four(const T* p, int valid) {
+  f32x4 r = {0.f, 0.f, 0.f, 0.f};
+  if (valid >= 4) {
+    if constexpr (sizeof(T) == 4) {
+      const u32x4 w = load_whole(p);
+      r = __builtin_bit_cast(f32x4, w);
+    } else {
+      const Bytes8 w = *reinterpret_cast<const Bytes8*>(p);
+      r = f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)};
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
+      if (q < valid) r[q] = Elem<T>::load(p + q);
+  }
   return r;
 }
 
@@ -294,8 +342,9 @@ template <typename T> __device__ __forceinline__ f32x4 multiply(const u32x4& b, 
   }
 }
 
-template <int TM_, int TN_, int WAVES_M_, int WAVES_N_> struct TileShape {
-  static constexpr int TM = TM_, TN = TN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_;
+// A tile of TM x TN by WAVES_M x WAVES_N wavefronts; RING: steps that LDS holds.
+template <int TM_, int TN_, int WAVES_M_, int WAVES_N_, int RING_ = 2> struct TileShape {
+  static constexpr int TM = TM_, TN = TN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, RING = RING_;
   static constexpr int THREADS = 64 * WAVES_M * WAVES_N;
   static constexpr int MI = TM / WAVES_M / 16, NI = TN / WAVES_N / 16;
 };
@@ -320,6 +369,9 @@ __device__ __forceinline__ void multiply_step(const char* la, const char* lb, f3
   }
 }
 
+// A point that no instruction is moved over.
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+
 // 16 bytes a lane from memory straight into LDS: lane l's land at base + 16 l (`base`: LDS byte address, the same in all
 // lanes).  Written as an instruction because the compiler, which sees LDS written by its own form of it, waits for all
 // copies before the next transposed read of LDS, also where that reads another buffer.  It has no result in registers;
@@ -331,11 +383,29 @@ __device__ __forceinline__ void copy_to_lds(const void* p, unsigned int base) {
 __device__ __forceinline__ unsigned int lds_address(const char* p) {
   return static_cast<unsigned int>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)p));
 }
-// All copies of this wavefront and its reads and writes of LDS are done; then the workgroup meets.
-__device__ __forceinline__ void meet_after_copies() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All but the N youngest copies of this wavefront and its reads and writes of LDS are done; then the workgroup meets.
+template <int N> __device__ __forceinline__ void meet_after_copies() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
 
-// A point that no instruction is moved over.
-__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+// The product of a tile by four wavefronts over `steps` steps of 128 bytes of the inner dimension, with RING steps in LDS:
+// issue(step, LDS address) copies a step's operands there, RING - 1 steps ahead of their product.
+template <typename T, class S, class A, class B, int RING, typename F, typename H>
+__device__ __forceinline__ void multiply_steps(char* lds, int steps, F&& issue, f32x4 (&acc)[S::MI][S::NI], H&& with_b) {
+  constexpr int BUFFER = A::BYTES + B::BYTES, COPIES = A::PER + B::PER;
+  const unsigned int at = lds_address(lds);
+  for (int step = 0; step < min(steps, RING - 1); ++step) issue(step, at + step * BUFFER);
+  int now = 0, then = RING - 1;
+  for (int step = 0; step < steps; ++step) {
+    // this step is in LDS, and the place of the one before is read to its end
+    if (step + RING - 1 <= steps) meet_after_copies<COPIES*(RING - 2)>();
+    else meet_after_copies<0>();
+    if (step + RING - 1 < steps) issue(step + RING - 1, at + then * BUFFER);
+    multiply_step<T, S, A, B>(lds + now * BUFFER, lds + now * BUFFER + A::BYTES, acc, with_b);
+    then = now;
+    now = now + 1 == RING ? 0 : now + 1;
+  }
+}
 
 // The product of a tile of 8 wavefronts, two on a SIMD, over `units` blocks of 32 inner indexes: issue(u, LDS address) copies
 // block u's operands to LDS, in COPIES instructions a wavefront.  The two wavefronts of a SIMD take turns: while one

@@ -71,8 +71,8 @@ bool whole_pieces(const void* data, int64_t ld, int32_t cols, int32_t dtype) {
   const int64_t per = 16 / dtype_size(dtype);
   return aligned(data, 16) && ld % per == 0 && cols % per == 0;
 }
-// Four results of a row in one access, or four times four in accesses of 16 bytes.
-bool whole_stores(const void* data, int64_t ld, int32_t dtype) { return aligned(data, 16) && ld % (16 / static_cast<int64_t>(dtype_size(dtype))) == 0; }
+// Rows that start on 16-byte boundaries.
+bool aligned_rows(const void* data, int64_t ld, int32_t dtype) { return aligned(data, 16) && ld % (16 / static_cast<int64_t>(dtype_size(dtype))) == 0; }
 
 // Splits of the inner dimension of the product that makes U: enough for two workgroups of 64 x 64 a compute unit, and at least
 // four steps each.
@@ -172,8 +172,8 @@ int lq_grouped_product(const lq_groups* groups, const lq_mat* X, int32_t x_slots
   a.slots = x_slots;
   a.x_grouped = (flags & LQ_X_GROUPED) != 0; a.y_grouped = (flags & LQ_Y_GROUPED) != 0;
   a.relu = (flags & LQ_RELU) != 0;
-  a.y_vec = whole_stores(Y->data, Y->ld, Y->dtype) && (!gate || whole_stores(gate->data, gate->ld, gate->dtype)) &&
-            (!bias || whole_stores(bias->data, bias->ld, bias->dtype));
+  a.y_vec = aligned_rows(Y->data, Y->ld, Y->dtype) && (!gate || aligned_rows(gate->data, gate->ld, gate->dtype)) &&
+            (!bias || aligned_rows(bias->data, bias->ld, bias->dtype));
   const int64_t per = 16 / static_cast<int64_t>(dtype_size(X->dtype));
   const bool in_vec = whole_pieces(X->data, X->ld, K, X->dtype) && whole_pieces(W->data, W->ld, W->cols, X->dtype) &&
                       (W->stride % per == 0 || groups->n_groups == 1);
@@ -209,8 +209,6 @@ int lq_grouped_gradient(const lq_groups* groups, const lq_mat* X, int32_t x_slot
   a.X = X->data; a.ldx = X->ld; a.slots = x_slots; a.x_grouped = (flags & LQ_X_GROUPED) != 0;
   a.dY = dY->data; a.ldy = dY->ld; a.y_grouped = (flags & LQ_Y_GROUPED) != 0;
   a.dW = dW->data; a.ldw = dW->ld; a.sw = dW->stride; a.w_bf16 = dW->dtype == LQ_BF16;
-  a.w_vec = whole_stores(dW->data, dW->ld, dW->dtype) && (dW->stride % 8 == 0 || groups->n_groups == 1) &&
-            (!db || whole_stores(db->data, db->ld, db->dtype));
   if (db) { a.db = db->data; a.ldb = db->ld; }
   a.k = X->cols; a.l = dY->cols;
   const bool in_vec = whole_pieces(X->data, X->ld, X->cols, X->dtype) && whole_pieces(dY->data, dY->ld, dY->cols, X->dtype);
@@ -273,7 +271,7 @@ int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W
   a.W = W->data; a.ldw = W->ld;
   if (bias) { a.bias = bias->data; a.ldb = bias->ld; }
   a.Y = Y->data; a.ldy = Y->ld; a.y_bf16 = Y->dtype == LQ_BF16; a.N = l; a.n_store = l;
-  a.y_vec = whole_stores(Y->data, Y->ld, Y->dtype) && (!bias || whole_stores(bias->data, bias->ld, bias->dtype));
+  a.y_vec = aligned_rows(Y->data, Y->ld, Y->dtype) && (!bias || aligned_rows(bias->data, bias->ld, bias->dtype));
   a.U = U; a.u_rest = n * rp; a.rp = rp; a.rank = rank;
   a.B = B->data; a.ldB = B->ld; a.sB = B->stride; a.group_of = group_of;
   const bool x_vec = whole_pieces(X->data, X->ld, k, dt);

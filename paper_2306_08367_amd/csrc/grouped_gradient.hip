@@ -14,20 +14,6 @@
 namespace lq {
 namespace {
 
-template <bool BF16> __device__ __forceinline__ void store_values(void* base, int64_t at, int valid, bool vec, f32x4 v) {
-  if (vec && valid >= 4) {
-    if constexpr (BF16) *reinterpret_cast<uint2*>(static_cast<bf16_t*>(base) + at) = uint2{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
-    else *reinterpret_cast<f32x4*>(static_cast<float*>(base) + at) = v;
-    return;
-  }
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
-    if (q < valid) {
-      if constexpr (BF16) static_cast<bf16_t*>(base)[at + q] = f32_to_bf16(v[q]);
-      else static_cast<float*>(base)[at + q] = v[q];
-    }
-}
-
 constexpr int SEGMENT = 2048;     // rows whose numbers are held in LDS at a time
 constexpr int RUN = 32;           // most tiles of a chunk that go to one die together
 
@@ -68,13 +54,13 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(Gradien
       for (int j = 0; j < S::NI; ++j) sum[j] = multiply<T>(b[j], ones, sum[j]);
   };
 
-  // (columns behind the last one repeat the last piece (direct copies) or are zeros; they are not stored)
+  // (columns behind the last one hold something else of the matrix or zeros; they are not stored)
   const T *X = static_cast<const T*>(a.X), *dY = static_cast<const T*>(a.dY);
   int ca[A::PER], cb[B::PER];
 #pragma unroll
-  for (int i = 0; i < A::PER; ++i) ca[i] = DIRECT ? min(m0 + A::piece_of(i) * EPC, a.k - EPC) : m0 + A::piece_of(i) * EPC;
+  for (int i = 0; i < A::PER; ++i) ca[i] = min(m0 + A::piece_of(i) * EPC, DIRECT ? a.k - EPC : a.k - 1);
 #pragma unroll
-  for (int i = 0; i < B::PER; ++i) cb[i] = DIRECT ? min(n0 + B::piece_of(i) * EPC, a.l - EPC) : n0 + B::piece_of(i) * EPC;
+  for (int i = 0; i < B::PER; ++i) cb[i] = min(n0 + B::piece_of(i) * EPC, DIRECT ? a.l - EPC : a.l - 1);
 
   for (int s0 = 0; s0 < chunk.rows; s0 += SEGMENT) {
     const int first = chunk.first + s0, rows = min(SEGMENT, chunk.rows - s0), steps = (rows + KSTEP - 1) / KSTEP;
@@ -85,8 +71,6 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(Gradien
       yrow[i] = a.y_grouped ? p : r;
     }
     __syncthreads();
-    auto x_row = [&](int line) { return X + xrow[line] * a.ldx; };
-    auto y_row = [&](int line) { return dY + yrow[line] * a.ldy; };
     // Where the pieces of a step lie (rows behind the last one: zeros in both operands).  Row numbers are read from LDS together
     // with operands and made addresses beside the products, a block ahead of their copies.
     constexpr int COPIES = A::PER + B::PER;
@@ -124,49 +108,77 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(Gradien
         locate();
       });
     } else if constexpr (DIRECT) {
-      issue(0, lds_address(lds));
-      for (int step = 0; step < steps; ++step) {
-        const int at = (step & 1) * BUFFER;
-        meet_after_copies();     // this buffer is whole, the other one is read to its end
-        if (step + 1 < steps) issue(step + 1, lds_address(lds) + (at ^ BUFFER));
-        multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc, add_up);
-      }
+      multiply_steps<T, S, A, B, S::RING>(lds, steps, issue, acc, [&](const u32x4(&b)[S::NI]) { add_up(b); });
     } else {
+      // A row may end inside a piece.  All 16 bytes may be read unless the row is the matrix's last one: there the 16 bytes end with
+      // the row, and are moved to their places on the way to LDS.  (Rows shorter than a piece: element by element.)
+      const bool narrow = a.k < EPC || a.l < EPC;
+      const int last_x = a.n / a.slots - 1, last_y = a.n - 1;
+      auto piece = [&](const T* base, int r, int64_t ld, int c, int cols, int last) -> const T* {
+        if (r < 0) return reinterpret_cast<const T*>(&g_zeros);
+        return base + r * ld + (r == last ? min(c, cols - EPC) : c);
+      };
+      auto in_place = [&](u32x4 v, int r, int c, int cols, int last) {
+        const int by = c - (cols - EPC);      // elements that it starts early
+        if (r == last && by > 0) {
+          const T* e = reinterpret_cast<const T*>(&v);
+          u32x4 w = {0, 0, 0, 0};
+#pragma unroll
+          for (int q = 0; q < EPC; ++q)
+#pragma unroll
+            for (int f = q + 1; f < EPC; ++f)
+              if (f == q + by) reinterpret_cast<T*>(&w)[q] = e[f];
+          return w;
+        }
+        return v;
+      };
+      auto x_at = [&](int line) { return line < rows ? xrow[line] : -1; };
+      auto y_at = [&](int line) { return line < rows ? yrow[line] : -1; };
       u32x4 ra[A::PER], rb[B::PER];
       auto fetch = [&](int step) {
 #pragma unroll
+        for (int i = 0; i < A::PER; ++i) ra[i] = load_whole(piece(X, x_at(step * KSTEP + A::line_of(i)), a.ldx, ca[i], a.k, last_x));
+#pragma unroll
+        for (int i = 0; i < B::PER; ++i) rb[i] = load_whole(piece(dY, y_at(step * KSTEP + B::line_of(i)), a.ldy, cb[i], a.l, last_y));
+      };
+      auto put = [&](int step, char* to) {
+#pragma unroll
+        for (int i = 0; i < A::PER; ++i)
+          *reinterpret_cast<u32x4*>(to + (i * THREADS + tid) * 16) = in_place(ra[i], x_at(step * KSTEP + A::line_of(i)), ca[i], a.k, last_x);
+#pragma unroll
+        for (int i = 0; i < B::PER; ++i)
+          *reinterpret_cast<u32x4*>(to + A::BYTES + (i * THREADS + tid) * 16) = in_place(rb[i], y_at(step * KSTEP + B::line_of(i)), cb[i], a.l, last_y);
+      };
+      auto fill = [&](int step, char* to) {
+#pragma unroll
         for (int i = 0; i < A::PER; ++i) {
-          const int line = step * KSTEP + A::line_of(i);
-          ra[i] = line < rows ? load_piece(x_row(line) + ca[i], a.k - ca[i]) : u32x4{0, 0, 0, 0};
+          const int r = x_at(step * KSTEP + A::line_of(i));
+          *reinterpret_cast<u32x4*>(to + (i * THREADS + tid) * 16) = load_piece(X + r * a.ldx + ca[i], r >= 0 ? a.k - ca[i] : 0);
         }
 #pragma unroll
         for (int i = 0; i < B::PER; ++i) {
-          const int line = step * KSTEP + B::line_of(i);
-          rb[i] = line < rows ? load_piece(y_row(line) + cb[i], a.l - cb[i]) : u32x4{0, 0, 0, 0};
+          const int r = y_at(step * KSTEP + B::line_of(i));
+          *reinterpret_cast<u32x4*>(to + A::BYTES + (i * THREADS + tid) * 16) = load_piece(dY + r * a.ldy + cb[i], r >= 0 ? a.l - cb[i] : 0);
         }
       };
-      auto put = [&](char* to) {
-#pragma unroll
-        for (int i = 0; i < A::PER; ++i) *reinterpret_cast<u32x4*>(to + (i * THREADS + tid) * 16) = ra[i];
-#pragma unroll
-        for (int i = 0; i < B::PER; ++i) *reinterpret_cast<u32x4*>(to + A::BYTES + (i * THREADS + tid) * 16) = rb[i];
-      };
-      fetch(0);
-      put(lds);
+      fill(0, lds);
       for (int step = 0; step < steps; ++step) {
         const int at = (step & 1) * BUFFER;
-        __syncthreads();         // likewise
-        if (step + 1 < steps) fetch(step + 1);
+        __syncthreads();         // this buffer is whole, the other one is read to its end
+        const bool more = step + 1 < steps, ahead = more && !narrow;
+        if (ahead) fetch(step + 1);
+        fence();                 // (the loads go ahead of the products)
         multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc, add_up);
-        if (step + 1 < steps) put(lds + (at ^ BUFFER));
+        if (ahead) put(step + 1, lds + (at ^ BUFFER));
+        else if (more) fill(step + 1, lds + (at ^ BUFFER));
       }
     }
   }
 
   const int64_t part = chunk.place >= 0 ? chunk.place * (static_cast<int64_t>(a.k) + 1) * a.l : 0;
   auto store = [&](void* base, int64_t at, int n, f32x4 v) {
-    if (a.w_bf16) store_values<true>(base, at + n, a.l - n, a.w_vec, v);
-    else store_values<false>(base, at + n, a.l - n, a.w_vec, v);
+    if (a.w_bf16) store_four<true>(base, at + n, a.l - n, v);
+    else store_four<false>(base, at + n, a.l - n, v);
   };
 #pragma unroll
   for (int j = 0; j < S::NI; ++j) {
@@ -176,11 +188,11 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(Gradien
     for (int i = 0; i < S::MI; ++i) {
       const int m = m0 + wm + 16 * i + (lane & 15);
       if (m >= a.k) continue;
-      if (chunk.place >= 0) store_values<false>(a.part, part + static_cast<int64_t>(m) * a.l + n, a.l - n, (a.l & 3) == 0, acc[i][j]);
+      if (chunk.place >= 0) store_four<false>(a.part, part + static_cast<int64_t>(m) * a.l + n, a.l - n, acc[i][j]);
       else store(a.dW, chunk.group * a.sw + m * a.ldw, n, acc[i][j]);
     }
     if (bias && (lane & 15) == 0) {
-      if (chunk.place >= 0) store_values<false>(a.part, part + static_cast<int64_t>(a.k) * a.l + n, a.l - n, (a.l & 3) == 0, sum[j]);
+      if (chunk.place >= 0) store_four<false>(a.part, part + static_cast<int64_t>(a.k) * a.l + n, a.l - n, sum[j]);
       else store(a.db, chunk.group * a.ldb, n, sum[j]);
     }
   }
@@ -236,16 +248,9 @@ template <bool BF16> __global__ __launch_bounds__(256) void gradient_sum_kernel(
     const float* p = a.part + first * stride + static_cast<int64_t>(m) * a.l + n;
     const int valid = min(4, a.l - n);
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if ((a.l & 3) == 0) {
-      for (int c = 0; c < count; ++c) v += *reinterpret_cast<const f32x4*>(p + c * stride);
-    } else {
-      for (int c = 0; c < count; ++c)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (q < valid) v[q] += p[c * stride + q];
-    }
-    if (m < a.k) store_values<BF16>(a.dW, group * a.sw + m * a.ldw + n, valid, a.w_vec, v);
-    else store_values<BF16>(a.db, group * a.ldb + n, valid, a.w_vec, v);
+    for (int c = 0; c < count; ++c) v += load_four(p + c * stride, valid);
+    if (m < a.k) store_four<BF16>(a.dW, group * a.sw + m * a.ldw + n, valid, v);
+    else store_four<BF16>(a.db, group * a.ldb + n, valid, v);
   }
 }
 
@@ -269,7 +274,7 @@ template <typename T, class S, bool DIRECT> int launch(GradientArgs a, const Pla
   constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
   typedef Operand<T, false, S::TM, S::THREADS, KBYTES> A;
   typedef Operand<T, false, S::TN, S::THREADS, KBYTES> B;
-  constexpr int LDS = (S::THREADS == 512 ? 4 : 2) * (A::BYTES + B::BYTES);
+  constexpr int LDS = (DIRECT ? S::RING : 2) * (A::BYTES + B::BYTES);
   a.tiles_m = (a.k + S::TM - 1) / S::TM;
   a.tiles_n = (a.l + S::TN - 1) / S::TN;
   const int64_t chunks = a.n / p.most + a.G, tiles = static_cast<int64_t>(a.tiles_m) * a.tiles_n;
@@ -285,8 +290,8 @@ template <typename T, class S, bool DIRECT> int launch(GradientArgs a, const Pla
 }
 
 typedef TileShape<128, 128, 2, 2> Tile128;
-typedef TileShape<64, 64, 2, 2> Tile64;
-typedef TileShape<256, 256, 2, 4> Tile256;
+typedef TileShape<64, 64, 2, 2, 4> Tile64;
+typedef TileShape<256, 256, 2, 4, 4> Tile256;
 
 template <typename T, bool DIRECT> int by_size(const GradientArgs& a, const Plan& p, hipStream_t s) {
   if constexpr (sizeof(T) == 2 && DIRECT)

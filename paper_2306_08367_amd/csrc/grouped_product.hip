@@ -15,39 +15,6 @@
 namespace lq {
 namespace {
 
-// The four values of a row from column n on, by the type that the call gives: bias, gate.
-template <typename T> __device__ __forceinline__ f32x4 load_four(const T* p, int valid, bool vec) {
-  f32x4 r = {0.f, 0.f, 0.f, 0.f};
-  if (vec) {
-    if constexpr (sizeof(T) == 4) {
-      r = *reinterpret_cast<const f32x4*>(p);
-    } else {
-      const uint2 w = *reinterpret_cast<const uint2*>(p);
-      r = f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
-                __uint_as_float(w.y & 0xffff0000u)};
-    }
-  } else {
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (q < valid) r[q] = Elem<T>::load(p + q);
-  }
-  return r;
-}
-
-__device__ __forceinline__ void store_four(void* row, int n, int valid, f32x4 v, bool bf16, bool vec) {
-  if (vec) {
-    if (bf16) *reinterpret_cast<uint2*>(static_cast<bf16_t*>(row) + n) = uint2{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
-    else *reinterpret_cast<f32x4*>(static_cast<float*>(row) + n) = v;
-    return;
-  }
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
-    if (q < valid) {
-      if (bf16) static_cast<bf16_t*>(row)[n + q] = f32_to_bf16(v[q]);
-      else static_cast<float*>(row)[n + q] = v[q];
-    }
-}
-
 // Bias, ReLU and gate, and the rows m of the tile for which stored(m).
 template <typename T, class S, typename F>
 __device__ __forceinline__ void store_tile(const GroupedArgs& a, const RowTile& tile, int n0, const int* yrow, f32x4 (&acc)[S::MI][S::NI], F&& stored) {
@@ -62,7 +29,7 @@ __device__ __forceinline__ void store_tile(const GroupedArgs& a, const RowTile& 
     f32x4 bv[4] = {};
     if (has_bias)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) bv[q] = load_four(bias + n + 4 * q, 4, true);
+      for (int q = 0; q < 4; ++q) bv[q] = load_four(bias + n + 4 * q, 4);
 #pragma unroll
     for (int i = 0; i < S::MI; ++i) {
       unsigned int v[4][4];
@@ -84,7 +51,7 @@ __device__ __forceinline__ void store_tile(const GroupedArgs& a, const RowTile& 
           y[j][q] = a.relu && x < 0.f ? 0.f : x;
         }
         if (a.gate) {
-          const f32x4 h = load_four(static_cast<const T*>(a.gate) + r * a.ldg + n + 4 * j, 4, true);
+          const f32x4 h = load_four(static_cast<const T*>(a.gate) + r * a.ldg + n + 4 * j, 4);
 #pragma unroll
           for (int q = 0; q < 4; ++q) y[j][q] = h[q] > 0.f ? y[j][q] : 0.f;
         }
@@ -107,9 +74,8 @@ __device__ __forceinline__ void store_tile(const GroupedArgs& a, const RowTile& 
   for (int j = 0; j < S::NI; ++j) {
     const int n = wn + 16 * j + 4 * (lane >> 4), valid = a.n_store - n;
     if (valid <= 0) continue;
-    const bool vec = a.y_vec && valid >= 4;
     f32x4 bv = {0.f, 0.f, 0.f, 0.f};
-    if (has_bias) bv = load_four(bias + n, a.N - n, vec);
+    if (has_bias) bv = load_four(bias + n, a.N - n);
 #pragma unroll
     for (int i = 0; i < S::MI; ++i) {
       const int m = wm + 16 * i + (lane & 15);
@@ -120,11 +86,12 @@ __device__ __forceinline__ void store_tile(const GroupedArgs& a, const RowTile& 
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = v[q] < 0.f ? 0.f : v[q];
       if (a.gate) {
-        const f32x4 h = load_four(static_cast<const T*>(a.gate) + r * a.ldg + n, valid, vec);
+        const f32x4 h = load_four(static_cast<const T*>(a.gate) + r * a.ldg + n, valid);
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = h[q] > 0.f ? v[q] : 0.f;
       }
-      store_four(Y + r * a.ldy * (a.y_bf16 ? 2 : 4), n, valid, v, a.y_bf16, vec);
+      if (a.y_bf16) store_four<true>(Y, r * a.ldy + n, valid, v);
+      else store_four<false>(Y, r * a.ldy + n, valid, v);
     }
   }
 }
@@ -191,7 +158,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
   const T* X = static_cast<const T*>(a.X);
   const T* W = static_cast<const T*>(a.W) + (any ? tile.group * a.sw : 0);
   // Where this thread's pieces of either operand lie at inner index 0, and their first inner index.  Columns behind the
-  // last one repeat the last piece (direct copies) or are zeros; they are not stored.
+  // last one hold something else of the matrix or zeros; they are not stored.
   const T *pa[A::PER], *pb[B::PER];
   int va[A::PER], vb[B::PER];
 #pragma unroll
@@ -203,7 +170,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
   for (int i = 0; i < B::PER; ++i) {
     const int line = B::line_of(i), e = B::piece_of(i) * EPC;
     vb[i] = BT ? e : line;
-    pb[i] = BT ? W + static_cast<int64_t>(min(n0 + line, a.N - 1)) * a.ldw + e : W + line * a.ldw + (DIRECT ? min(n0 + e, a.N - EPC) : n0 + e);
+    pb[i] = BT ? W + static_cast<int64_t>(min(n0 + line, a.N - 1)) * a.ldw + e : W + line * a.ldw + min(n0 + e, DIRECT ? a.N - EPC : a.N - 1);
   }
   const int64_t step_b = BT ? 1 : a.ldw;     // elements per inner index
   constexpr int BUFFER = A::BYTES + B::BYTES, SLOTS = KSTEP / EPC;
@@ -253,31 +220,47 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
         copy_to_lds(k0 + vb[i] < k_end ? static_cast<const void*>(pb[i] + k0 * step_b) : &g_zeros, to + A::BYTES + i * THREADS * 16);
     }
   };
+  // Up to here all 16 bytes of a piece may be read: a row of X ends behind it; a row of W may end inside it, but another follows.
+  const int whole_end = BT ? k_end : a.ldw >= EPC ? min(k_end, a.K - 1) : 0;
+  auto whole = [&](int step) { return step < own_steps && k_first + (step + 1) * KSTEP <= whole_end; };
   u32x4 ra[DIRECT ? 1 : A::PER], rb[DIRECT ? 1 : B::PER];
   auto fetch = [&](int step) {
     const int k0 = k_first + step * KSTEP;
-    if (ADAPT && step >= own_steps) {
 #pragma unroll
-      for (int i = 0; i < A::PER; ++i) ra[i] = *static_cast<const u32x4*>(piece_of_u(step, i));
+    for (int i = 0; i < A::PER; ++i) ra[i] = load_whole(pa[i] + k0);
 #pragma unroll
-      for (int i = 0; i < B::PER; ++i) {
-        const T* row = row_of_b(step, i);
-        const int n = n0 + B::piece_of(i) * EPC;
-        rb[i] = load_piece(row + n, row ? a.N - n : 0);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < A::PER; ++i) ra[i] = load_piece(pa[i] + k0, k_end - (k0 + va[i]));
-#pragma unroll
-      for (int i = 0; i < B::PER; ++i)
-        rb[i] = load_piece(pb[i] + k0 * step_b, BT ? k_end - (k0 + vb[i]) : k0 + vb[i] < k_end ? a.N - n0 - B::piece_of(i) * EPC : 0);
-    }
+    for (int i = 0; i < B::PER; ++i) rb[i] = load_whole(pb[i] + k0 * step_b);
   };
   auto put = [&](char* to) {
 #pragma unroll
     for (int i = 0; i < A::PER; ++i) *reinterpret_cast<u32x4*>(to + (i * THREADS + tid) * 16) = ra[i];
 #pragma unroll
     for (int i = 0; i < B::PER; ++i) *reinterpret_cast<u32x4*>(to + A::BYTES + (i * THREADS + tid) * 16) = rb[i];
+  };
+  // A step that is not whole, from memory to LDS at once (its loads beside the products of the step before would meet those of
+  // the other kind in the same registers, and the compiler would wait for both there).
+  auto fill = [&](int step, char* to) {
+    const int k0 = k_first + step * KSTEP;
+    const bool of_adapters = ADAPT && step >= own_steps;
+#pragma unroll
+    for (int i = 0; i < A::PER; ++i) {
+      u32x4 v;
+      if (of_adapters) v = *static_cast<const u32x4*>(piece_of_u(step, i));
+      else v = load_piece(pa[i] + k0, k_end - (k0 + va[i]));
+      *reinterpret_cast<u32x4*>(to + (i * THREADS + tid) * 16) = v;
+    }
+#pragma unroll
+    for (int i = 0; i < B::PER; ++i) {
+      const int n = n0 + B::piece_of(i) * EPC;
+      u32x4 v;
+      if (of_adapters) {
+        const T* row = row_of_b(step, i);
+        v = load_piece(row + n, row ? a.N - n : 0);
+      } else {
+        v = load_piece(pb[i] + k0 * step_b, BT ? k_end - (k0 + vb[i]) : k0 + vb[i] < k_end ? a.N - n : 0);
+      }
+      *reinterpret_cast<u32x4*>(to + A::BYTES + (i * THREADS + tid) * 16) = v;
+    }
   };
 
   const auto nothing = [](const u32x4(&)[S::NI]) {};
@@ -291,22 +274,18 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
       if constexpr (DIRECT && THREADS == 512) {
         multiply_in_turns<T, S, A, B>(lds, steps, issue, acc, nothing);
       } else if constexpr (DIRECT) {
-        issue(0, lds_address(lds));
-        for (int step = 0; step < steps; ++step) {
-          const int at = (step & 1) * BUFFER;
-          meet_after_copies();     // this buffer is whole, the other one is read to its end
-          if (step + 1 < steps) issue(step + 1, lds_address(lds) + (at ^ BUFFER));
-          multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc, nothing);
-        }
+        multiply_steps<T, S, A, B, S::RING>(lds, steps, issue, acc, nothing);
       } else {
-        fetch(0);
-        put(lds);
+        fill(0, lds);
         for (int step = 0; step < steps; ++step) {
           const int at = (step & 1) * BUFFER;
-          __syncthreads();         // likewise
-          if (step + 1 < steps) fetch(step + 1);
+          __syncthreads();         // this buffer is whole, the other one is read to its end
+          const bool more = step + 1 < steps, ahead = more && whole(step + 1);
+          if (ahead) fetch(step + 1);
+          fence();                 // (the loads go ahead of the products)
           multiply_step<T, S, A, B>(lds + at, lds + at + A::BYTES, acc, nothing);
-          if (step + 1 < steps) put(lds + (at ^ BUFFER));
+          if (ahead) put(lds + (at ^ BUFFER));
+          else if (more) fill(step + 1, lds + (at ^ BUFFER));
         }
       }
     }
@@ -342,7 +321,7 @@ template <typename T, class S, bool BT, bool DIRECT, bool ADAPT> int launch(Grou
   constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
   typedef Operand<T, true, S::TM, S::THREADS, KBYTES> A;
   typedef Operand<T, BT, S::TN, S::THREADS, KBYTES> B;
-  constexpr int LDS = (S::THREADS == 512 ? 4 : 2) * (A::BYTES + B::BYTES);
+  constexpr int LDS = (DIRECT ? S::RING : 2) * (A::BYTES + B::BYTES);
   a.tiles_n = (a.n_store + S::TN - 1) / S::TN;
   a.row_tiles = ADAPT ? (a.n + S::TM - 1) / S::TM : a.n / S::TM + std::min(a.n, a.G + 1);
   const int steps = (a.K + A::KSTEP - 1) / A::KSTEP;
@@ -359,13 +338,19 @@ template <typename T, class S, bool BT, bool DIRECT, bool ADAPT> int launch(Grou
 
 typedef TileShape<128, 128, 2, 2> Tile128;
 typedef TileShape<64, 64, 2, 2> Tile64;
-typedef TileShape<256, 256, 2, 4> Tile256;
+typedef TileShape<64, 64, 2, 2, 4> Tile64Ahead;
+typedef TileShape<256, 256, 2, 4, 4> Tile256;
 
 template <typename T, bool BT, bool DIRECT, bool ADAPT> int by_size(const GroupedArgs& a, int splits, hipStream_t s) {
   const int64_t large = static_cast<int64_t>((a.n_store + 127) / 128) * ((a.n + 127) / 128);
   if constexpr (sizeof(T) == 2 && DIRECT)
     if (large >= 4 * num_cus()) return launch<T, Tile256, BT, DIRECT, ADAPT>(a, splits, s);
   if (large >= num_cus()) return launch<T, Tile128, BT, DIRECT, ADAPT>(a, splits, s);
+  // Few tiles: three steps ahead in each instead of several workgroups a compute unit (64 rows, 4,096 -> 4,096 with adapters: 59 -> 44 us;
+  // 1,024 tiles of 64 experts' matrices, 2,048 -> 1,024: 45 us three steps ahead, 38 one).
+  const int64_t small = static_cast<int64_t>((a.n_store + 63) / 64) * ((a.n + 63) / 64 + (ADAPT ? 0 : std::min(a.n, a.G) / 2)) * splits;
+  if constexpr (DIRECT)
+    if (small < 3 * num_cus()) return launch<T, Tile64Ahead, BT, DIRECT, ADAPT>(a, splits, s);
   return launch<T, Tile64, BT, DIRECT, ADAPT>(a, splits, s);
 }
 
