@@ -51,13 +51,13 @@ int launch_group_rows(const int32_t* keys, int64_t n, int32_t G, int32_t* off, i
 size_t group_rows_ws_bytes(int64_t n, int32_t G);
 int launch_check_groups(const lq_groups& g, int32_t* flag, hipStream_t s);
 int launch_check_keys(const int32_t* keys, int64_t n, int32_t G, int32_t* flag, hipStream_t s);
-// `in_vec`: rows of X and of the matrices may be read in aligned 16-byte pieces.
-int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed, bool in_vec, hipStream_t s);
+// `copy`: rows of X and of the matrices may be read in pieces of 16 or 4 bytes, aligned to that, or only element by element (0).
+int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed, int copy, hipStream_t s);
 // `low` makes the partial sums of U (in low.Y, `splits` of them), `u` holds U itself.
-int launch_adapter_product(const GroupedArgs& main, const GroupedArgs& low, int splits, const float* scale, void* u, int32_t dtype, bool main_vec,
-                           bool low_vec, hipStream_t s);
+int launch_adapter_product(const GroupedArgs& main, const GroupedArgs& low, int splits, const float* scale, void* u, int32_t dtype, int main_copy,
+                           int low_copy, hipStream_t s);
 size_t grouped_gradient_ws_bytes(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype);
-int launch_grouped_gradient(const GradientArgs& a, int32_t dtype, bool in_vec, void* ws, size_t ws_bytes, hipStream_t s);
+int launch_grouped_gradient(const GradientArgs& a, int32_t dtype, int copy, void* ws, size_t ws_bytes, hipStream_t s);
 
 #ifdef __HIPCC__
 
@@ -279,15 +279,17 @@ __device__ __forceinline__ Chunk find_chunk(const int32_t* __restrict__ off, int
 //   !KMAJ   a line per inner index, the rows along it: bf16 operands come transposed out of LDS
 //           (ds_read_b64_tr_b16: four inner indexes of a row a lane), fp32 ones a word at a time
 // Piece c of a line lies at place c ^ spread(line), so that the lanes of a read use all banks.
-template <typename T, bool KMAJ, int EXT, int THREADS, int KBYTES = 128> struct Operand {
+// COPY: bytes that a lane brings at a time (16, or 4 where rows are aligned to that only).
+template <typename T, bool KMAJ, int EXT, int THREADS, int KBYTES = 128, int COPY = 16> struct Operand {
   static constexpr int EPC = 16 / sizeof(T);
   static constexpr int KSTEP = KBYTES / sizeof(T);
   static constexpr int LINES = KMAJ ? EXT : KSTEP;
   static constexpr int CPL = KMAJ ? KBYTES / 16 : EXT / EPC;
   static constexpr int PIECES = LINES * CPL;
-  static constexpr int PER = PIECES / THREADS;
   static constexpr int BYTES = PIECES * 16;
-  static_assert(PIECES % THREADS == 0, "whole pieces a thread");
+  static constexpr int PER = BYTES / COPY / THREADS;      // copies of a thread
+  static constexpr int CPP = 16 / COPY;                   // of a piece
+  static_assert(BYTES % (COPY * THREADS) == 0, "whole copies a thread");
 
   static __device__ __forceinline__ int spread(int line) {
     if constexpr (KMAJ) return CPL == 8 ? (line >> 1) & 7 : (line >> 2) & 3;
@@ -295,11 +297,11 @@ template <typename T, bool KMAJ, int EXT, int THREADS, int KBYTES = 128> struct 
     else if constexpr (CPL >= 16) return 2 * ((line & 3) | ((line >> 1) & 4));
     else return 2 * (((line >> 1) & 1) | ((line >> 2) & 2));
   }
-  static __device__ __forceinline__ int line_of(int i) { return (i * THREADS + static_cast<int>(threadIdx.x)) / CPL; }
-  // the piece of its line that thread's i-th place holds
-  static __device__ __forceinline__ int piece_of(int i) {
-    const int id = i * THREADS + threadIdx.x;
-    return (id % CPL) ^ spread(id / CPL);
+  // The line of the thread's i-th copy, and the element of it that it begins with.
+  static __device__ __forceinline__ int line_of(int i) { return (i * THREADS + static_cast<int>(threadIdx.x)) / (CPL * CPP); }
+  static __device__ __forceinline__ int element_of(int i) {
+    const int id = i * THREADS + threadIdx.x, at = id % (CPL * CPP);
+    return ((at / CPP) ^ spread(id / (CPL * CPP))) * EPC + at % CPP * (COPY / static_cast<int>(sizeof(T)));
   }
   static __device__ __forceinline__ int place(int line, int piece) { return (line * CPL + (piece ^ spread(line))) * 16; }
 
@@ -372,13 +374,15 @@ __device__ __forceinline__ void multiply_step(const char* la, const char* lb, f3
 // A point that no instruction is moved over.
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
-// 16 bytes a lane from memory straight into LDS: lane l's land at base + 16 l (`base`: LDS byte address, the same in all
+// COPY (16 or 4) bytes a lane from memory straight into LDS: lane l's land at base + COPY l (`base`: LDS byte address, the same in all
 // lanes).  Written as an instruction because the compiler, which sees LDS written by its own form of it, waits for all
 // copies before the next transposed read of LDS, also where that reads another buffer.  It has no result in registers;
 // the compiler does not count it: meet_after_copies() waits for it.  It writes m0, which nothing else in these kernels
 // uses (the compiler takes no m0 in a list of what an instruction overwrites; a test reads the assembly for it).
-__device__ __forceinline__ void copy_to_lds(const void* p, unsigned int base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(base)), "v"(p));
+template <int COPY> __device__ __forceinline__ void copy_to_lds(const void* p, unsigned int base) {
+  base = __builtin_amdgcn_readfirstlane(base);
+  if constexpr (COPY == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(base), "v"(p));
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(base), "v"(p));
 }
 __device__ __forceinline__ unsigned int lds_address(const char* p) {
   return static_cast<unsigned int>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)p));

@@ -66,11 +66,15 @@ int verify_groups(const lq_groups& g, uint32_t flags, void* ws, size_t ws_bytes,
   return LQ_OK;
 }
 
-// Rows that start on 16-byte boundaries and end on one.
-bool whole_pieces(const void* data, int64_t ld, int32_t cols, int32_t dtype) {
-  const int64_t per = 16 / dtype_size(dtype);
-  return aligned(data, 16) && ld % per == 0 && cols % per == 0;
+// The pieces (16 or 4 bytes, 0: elements of two) in which rows may be read: they start and end on boundaries of those.
+int piece_bytes(const void* data, int64_t ld, int32_t cols, int64_t stride, int32_t dtype) {
+  const int64_t size = static_cast<int64_t>(dtype_size(dtype));
+  for (const int bytes : {16, 4})
+    if (aligned(data, bytes) && ld * size % bytes == 0 && cols * size % bytes == 0 && stride * size % bytes == 0) return bytes;
+  return 0;
 }
+int piece_bytes(const lq_mat& m) { return piece_bytes(m.data, m.ld, m.cols, 0, m.dtype); }
+int piece_bytes(const lq_stack& w) { return piece_bytes(w.data, w.ld, w.cols, w.count > 1 ? w.stride : 0, w.dtype); }
 // Rows that start on 16-byte boundaries.
 bool aligned_rows(const void* data, int64_t ld, int32_t dtype) { return aligned(data, 16) && ld % (16 / static_cast<int64_t>(dtype_size(dtype))) == 0; }
 
@@ -174,10 +178,7 @@ int lq_grouped_product(const lq_groups* groups, const lq_mat* X, int32_t x_slots
   a.relu = (flags & LQ_RELU) != 0;
   a.y_vec = aligned_rows(Y->data, Y->ld, Y->dtype) && (!gate || aligned_rows(gate->data, gate->ld, gate->dtype)) &&
             (!bias || aligned_rows(bias->data, bias->ld, bias->dtype));
-  const int64_t per = 16 / static_cast<int64_t>(dtype_size(X->dtype));
-  const bool in_vec = whole_pieces(X->data, X->ld, K, X->dtype) && whole_pieces(W->data, W->ld, W->cols, X->dtype) &&
-                      (W->stride % per == 0 || groups->n_groups == 1);
-  return launch_grouped_product(a, X->dtype, transposed, in_vec, s);
+  return launch_grouped_product(a, X->dtype, transposed, std::min(piece_bytes(*X), piece_bytes(*W)), s);
 }
 
 int lq_grouped_gradient(const lq_groups* groups, const lq_mat* X, int32_t x_slots, const lq_mat* dY, lq_stack* dW, lq_mat* db,
@@ -211,9 +212,8 @@ int lq_grouped_gradient(const lq_groups* groups, const lq_mat* X, int32_t x_slot
   a.dW = dW->data; a.ldw = dW->ld; a.sw = dW->stride; a.w_bf16 = dW->dtype == LQ_BF16;
   if (db) { a.db = db->data; a.ldb = db->ld; }
   a.k = X->cols; a.l = dY->cols;
-  const bool in_vec = whole_pieces(X->data, X->ld, X->cols, X->dtype) && whole_pieces(dY->data, dY->ld, dY->cols, X->dtype);
   if (ws && !aligned(ws, 256)) return fail(LQ_ERR_WORKSPACE, "lq_grouped_gradient: the workspace is not 256-byte aligned");
-  return launch_grouped_gradient(a, X->dtype, in_vec, ws, ws_bytes, s);
+  return launch_grouped_gradient(a, X->dtype, std::min(piece_bytes(*X), piece_bytes(*dY)), ws, ws_bytes, s);
 }
 
 size_t lq_adapter_workspace_bytes(int64_t n, int32_t n_groups, int32_t k, int32_t l, int32_t rank, int32_t dtype) {
@@ -259,8 +259,6 @@ int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W
   char* part = static_cast<char*>(ws) + 256;
   char* U = part + adapter_u_bytes(n, rp, splits);
   int32_t* group_of = reinterpret_cast<int32_t*>(U + adapter_u_bytes(n, rp, 1));
-  const int64_t per = 16 / static_cast<int64_t>(dtype_size(dt));
-
   GroupedArgs a{};
   a.off = groups->offsets; a.order = groups->order; a.G = groups->n_groups; a.n = static_cast<int32_t>(n);
   a.X = X->data; a.ldx = X->ld; a.K = k; a.slots = 1;
@@ -274,11 +272,8 @@ int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W
   a.y_vec = aligned_rows(Y->data, Y->ld, Y->dtype) && (!bias || aligned_rows(bias->data, bias->ld, bias->dtype));
   a.U = U; a.u_rest = n * rp; a.rp = rp; a.rank = rank;
   a.B = B->data; a.ldB = B->ld; a.sB = B->stride; a.group_of = group_of;
-  const bool x_vec = whole_pieces(X->data, X->ld, k, dt);
-  const bool main_vec = x_vec && whole_pieces(W->data, W->ld, l, dt) && whole_pieces(B->data, B->ld, l, dt) &&
-                        (B->stride % per == 0 || groups->n_groups == 1);
-  const bool low_vec = x_vec && whole_pieces(A->data, A->ld, rank, dt) && (A->stride % per == 0 || groups->n_groups == 1);
-  return launch_adapter_product(a, low, splits, scale, U, dt, main_vec, low_vec, s);
+  const int of_x = piece_bytes(*X);
+  return launch_adapter_product(a, low, splits, scale, U, dt, std::min({of_x, piece_bytes(*W), piece_bytes(*B)}), std::min(of_x, piece_bytes(*A)), s);
 }
 
 }  // extern "C"

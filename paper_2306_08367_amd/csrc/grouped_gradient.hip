@@ -17,11 +17,13 @@ namespace {
 constexpr int SEGMENT = 2048;     // rows whose numbers are held in LDS at a time
 constexpr int RUN = 32;           // most tiles of a chunk that go to one die together
 
-template <typename T, class S, bool DIRECT>
+template <typename T, class S, int COPY>
 __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(GradientArgs a) {
   constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
-  typedef Operand<T, false, S::TM, S::THREADS, KBYTES> A;
-  typedef Operand<T, false, S::TN, S::THREADS, KBYTES> B;
+  typedef Operand<T, false, S::TM, S::THREADS, KBYTES, COPY ? COPY : 16> A;
+  typedef Operand<T, false, S::TN, S::THREADS, KBYTES, COPY ? COPY : 16> B;
+  constexpr bool DIRECT = COPY != 0;           // through LDS without registers
+  constexpr int E = DIRECT ? COPY / static_cast<int>(sizeof(T)) : 1;
   constexpr int KSTEP = A::KSTEP, EPC = A::EPC, THREADS = S::THREADS, BUFFER = A::BYTES + B::BYTES;
   extern __shared__ __align__(1024) char lds[];
   __shared__ int xrow[SEGMENT], yrow[SEGMENT];
@@ -58,9 +60,9 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(Gradien
   const T *X = static_cast<const T*>(a.X), *dY = static_cast<const T*>(a.dY);
   int ca[A::PER], cb[B::PER];
 #pragma unroll
-  for (int i = 0; i < A::PER; ++i) ca[i] = min(m0 + A::piece_of(i) * EPC, DIRECT ? a.k - EPC : a.k - 1);
+  for (int i = 0; i < A::PER; ++i) ca[i] = min(m0 + A::element_of(i), a.k - E);
 #pragma unroll
-  for (int i = 0; i < B::PER; ++i) cb[i] = min(n0 + B::piece_of(i) * EPC, DIRECT ? a.l - EPC : a.l - 1);
+  for (int i = 0; i < B::PER; ++i) cb[i] = min(n0 + B::element_of(i), a.l - E);
 
   for (int s0 = 0; s0 < chunk.rows; s0 += SEGMENT) {
     const int first = chunk.first + s0, rows = min(SEGMENT, chunk.rows - s0), steps = (rows + KSTEP - 1) / KSTEP;
@@ -99,8 +101,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(Gradien
       }
 #pragma unroll
       for (int c = 0; c < COPIES; ++c)
-        copy_to_lds(from[c], to + wave * 1024 + (c >= A::PER ? A::BYTES + (c - A::PER) * THREADS * 16 : c * THREADS * 16));
-      look_up(step + 1);
+        copy_to_lds<COPY>(from[c], to + wave * 64 * COPY + (c >= A::PER ? A::BYTES + (c - A::PER) * THREADS * COPY : c * THREADS * COPY));
+      if constexpr (THREADS == 512) look_up(step + 1);
     };
     if constexpr (DIRECT && THREADS == 512) {
       multiply_in_turns<T, S, A, B>(lds, steps, issue, acc, [&](const u32x4(&b)[S::NI]) {
@@ -248,7 +250,15 @@ template <bool BF16> __global__ __launch_bounds__(256) void gradient_sum_kernel(
     const float* p = a.part + first * stride + static_cast<int64_t>(m) * a.l + n;
     const int valid = min(4, a.l - n);
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int c = 0; c < count; ++c) v += load_four(p + c * stride, valid);
+    int c = 0;
+    for (; c + 4 <= count; c += 4) {      // (four loads under way together)
+      f32x4 w[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) w[q] = load_four(p + (c + q) * stride, valid);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v += w[q];
+    }
+    for (; c < count; ++c) v += load_four(p + c * stride, valid);
     if (m < a.k) store_four<BF16>(a.dW, group * a.sw + m * a.ldw + n, valid, v);
     else store_four<BF16>(a.db, group * a.ldb + n, valid, v);
   }
@@ -258,9 +268,9 @@ template <bool BF16> __global__ __launch_bounds__(256) void gradient_sum_kernel(
 // is filled, in bf16 with aligned rows.  A workgroup's share of n rows is n * tiles / workgroups that run at once (one of 512
 // threads a compute unit, else two).
 struct Plan { int side; int64_t most, places; };
-Plan plan_of(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype, bool in_vec) {
+Plan plan_of(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype, int copy) {
   Plan p;
-  p.side = dtype == LQ_BF16 && in_vec && k > 192 && l > 192 ? 256 : k > 64 && l > 64 ? 128 : 64;
+  p.side = dtype == LQ_BF16 && copy == 16 && k > 192 && l > 192 ? 256 : k > 64 && l > 64 ? 128 : 64;
   const int64_t tiles = static_cast<int64_t>((k + p.side - 1) / p.side) * ((l + p.side - 1) / p.side);
   const int64_t even = n * tiles / (num_cus() * (p.side == 256 ? 1 : 2));
   p.most = std::max<int64_t>((even + 63) / 64 * 64, dtype == LQ_BF16 ? 1024 : 256);
@@ -270,18 +280,18 @@ Plan plan_of(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype, bool in_
 }
 size_t place_bytes(int64_t places, int32_t k, int32_t l) { return static_cast<size_t>(places) * (static_cast<size_t>(k) + 1) * l * 4; }
 
-template <typename T, class S, bool DIRECT> int launch(GradientArgs a, const Plan& p, hipStream_t s) {
+template <typename T, class S, int COPY> int launch(GradientArgs a, const Plan& p, hipStream_t s) {
   constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
-  typedef Operand<T, false, S::TM, S::THREADS, KBYTES> A;
-  typedef Operand<T, false, S::TN, S::THREADS, KBYTES> B;
-  constexpr int LDS = (DIRECT ? S::RING : 2) * (A::BYTES + B::BYTES);
+  typedef Operand<T, false, S::TM, S::THREADS, KBYTES, COPY ? COPY : 16> A;
+  typedef Operand<T, false, S::TN, S::THREADS, KBYTES, COPY ? COPY : 16> B;
+  constexpr int LDS = (COPY ? S::RING : 2) * (A::BYTES + B::BYTES);
   a.tiles_m = (a.k + S::TM - 1) / S::TM;
   a.tiles_n = (a.l + S::TN - 1) / S::TN;
   const int64_t chunks = a.n / p.most + a.G, tiles = static_cast<int64_t>(a.tiles_m) * a.tiles_n;
   const int64_t run_tiles = std::min<int64_t>(tiles, RUN), runs = chunks * ((tiles + run_tiles - 1) / run_tiles);
   const int64_t blocks = (runs + 7) / 8 * 8 * run_tiles;
   if (blocks > 0x7fffffff) return fail(LQ_ERR_UNSUPPORTED, "grouped gradient: %lld tiles are more than one launch takes", (long long)blocks);
-  const auto kernel = grouped_gradient_kernel<T, S, DIRECT>;
+  const auto kernel = grouped_gradient_kernel<T, S, COPY>;
   if (LDS + SEGMENT * 4 > 48 * 1024)
     LQ_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
   kernel<<<static_cast<unsigned>(blocks), S::THREADS, LDS, s>>>(a);
@@ -293,29 +303,33 @@ typedef TileShape<128, 128, 2, 2> Tile128;
 typedef TileShape<64, 64, 2, 2, 4> Tile64;
 typedef TileShape<256, 256, 2, 4, 4> Tile256;
 
-template <typename T, bool DIRECT> int by_size(const GradientArgs& a, const Plan& p, hipStream_t s) {
-  if constexpr (sizeof(T) == 2 && DIRECT)
-    if (p.side == 256) return launch<T, Tile256, DIRECT>(a, p, s);
-  return p.side == 128 ? launch<T, Tile128, DIRECT>(a, p, s) : launch<T, Tile64, DIRECT>(a, p, s);
+template <typename T, int COPY> int by_size(const GradientArgs& a, const Plan& p, hipStream_t s) {
+  if constexpr (sizeof(T) == 2 && COPY == 16)
+    if (p.side == 256) return launch<T, Tile256, COPY>(a, p, s);
+  return p.side == 128 ? launch<T, Tile128, COPY>(a, p, s) : launch<T, Tile64, COPY>(a, p, s);
+}
+template <typename T> int by_copy(const GradientArgs& a, int copy, const Plan& p, hipStream_t s) {
+  if (copy == 16) return by_size<T, 16>(a, p, s);
+  if constexpr (sizeof(T) == 2)
+    if (copy == 0) return by_size<T, 0>(a, p, s);
+  return by_size<T, 4>(a, p, s);
 }
 
 }  // namespace
 
 size_t grouped_gradient_ws_bytes(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype) {
   size_t most = 0;
-  for (const bool in_vec : {false, true}) most = std::max(most, place_bytes(plan_of(n, G, k, l, dtype, in_vec).places, k, l));
+  for (const int copy : {4, 16}) most = std::max(most, place_bytes(plan_of(n, G, k, l, dtype, copy).places, k, l));
   return round_up(most, 256);
 }
 
-int launch_grouped_gradient(const GradientArgs& args, int32_t dtype, bool in_vec, void* ws, size_t ws_bytes, hipStream_t s) {
+int launch_grouped_gradient(const GradientArgs& args, int32_t dtype, int copy, void* ws, size_t ws_bytes, hipStream_t s) {
   GradientArgs a = args;
-  Plan p = plan_of(a.n, a.G, a.k, a.l, dtype, in_vec);
+  Plan p = plan_of(a.n, a.G, a.k, a.l, dtype, copy);
   if (!ws || ws_bytes < place_bytes(p.places, a.k, a.l)) p.most = std::max<int64_t>(a.n, 1);     // without room: whole groups
   a.most = static_cast<int32_t>(p.most);
   a.part = static_cast<float*>(ws);
-  int rc;
-  if (dtype == LQ_BF16) rc = in_vec ? by_size<bf16_t, true>(a, p, s) : by_size<bf16_t, false>(a, p, s);
-  else rc = in_vec ? by_size<float, true>(a, p, s) : by_size<float, false>(a, p, s);
+  const int rc = dtype == LQ_BF16 ? by_copy<bf16_t>(a, copy, p, s) : by_copy<float>(a, copy, p, s);
   if (rc) return rc;
   if (a.n > p.most) {
     const int64_t fours = static_cast<int64_t>(a.k + 1) * ((a.l + 3) / 4);

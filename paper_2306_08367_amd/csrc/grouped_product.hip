@@ -96,12 +96,14 @@ __device__ __forceinline__ void store_tile(const GroupedArgs& a, const RowTile& 
   }
 }
 
-template <typename T, class S, bool BT, bool DIRECT, bool ADAPT>
+template <typename T, class S, bool BT, int COPY, bool ADAPT>
 __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedArgs a) {
   constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
-  typedef Operand<T, true, S::TM, S::THREADS, KBYTES> A;
-  typedef Operand<T, BT, S::TN, S::THREADS, KBYTES> B;
+  typedef Operand<T, true, S::TM, S::THREADS, KBYTES, COPY ? COPY : 16> A;
+  typedef Operand<T, BT, S::TN, S::THREADS, KBYTES, COPY ? COPY : 16> B;
+  constexpr bool DIRECT = COPY != 0;           // through LDS without registers
   constexpr int KSTEP = A::KSTEP, EPC = A::EPC, THREADS = S::THREADS;
+  constexpr int E = DIRECT ? COPY / static_cast<int>(sizeof(T)) : 1;
   extern __shared__ __align__(1024) char lds[];
   __shared__ int xrow[S::TM], yrow[S::TM];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -163,14 +165,14 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
   int va[A::PER], vb[B::PER];
 #pragma unroll
   for (int i = 0; i < A::PER; ++i) {
-    va[i] = A::piece_of(i) * EPC;
+    va[i] = A::element_of(i);
     pa[i] = X + xrow[A::line_of(i)] * a.ldx + va[i];
   }
 #pragma unroll
   for (int i = 0; i < B::PER; ++i) {
-    const int line = B::line_of(i), e = B::piece_of(i) * EPC;
+    const int line = B::line_of(i), e = B::element_of(i);
     vb[i] = BT ? e : line;
-    pb[i] = BT ? W + static_cast<int64_t>(min(n0 + line, a.N - 1)) * a.ldw + e : W + line * a.ldw + min(n0 + e, DIRECT ? a.N - EPC : a.N - 1);
+    pb[i] = BT ? W + static_cast<int64_t>(min(n0 + line, a.N - 1)) * a.ldw + e : W + line * a.ldw + min(n0 + e, a.N - E);
   }
   const int64_t step_b = BT ? 1 : a.ldw;     // elements per inner index
   constexpr int BUFFER = A::BYTES + B::BYTES, SLOTS = KSTEP / EPC;
@@ -181,9 +183,10 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
   const int steps = own_steps + (ADAPT ? (2 * adapters * per + SLOTS - 1) / SLOTS : 0);
   int only = -1;      // >= 0: of this adapter's pieces alone
   auto piece_of_u = [&](int step, int i) -> const void* {
-    const int qq = (step - own_steps) * SLOTS + va[i] / EPC, q = qq >> 1, ad = q / per, line = A::line_of(i);
+    const int line = A::line_of(i), e = A::element_of(i);
+    const int qq = (step - own_steps) * SLOTS + e / EPC, q = qq >> 1, ad = q / per;
     if (which[line] != ad || (only >= 0 && only != ad)) return &g_zeros;
-    const int64_t at = static_cast<int64_t>(tile.first + line) * a.rp + (q - ad * per) * 8;
+    const int64_t at = static_cast<int64_t>(tile.first + line) * a.rp + (q - ad * per) * 8 + e % EPC;
     if constexpr (sizeof(T) == 2) return static_cast<const bf16_t*>(a.U) + ((qq & 1) ? a.u_rest : 0) + at;
     else return static_cast<const float*>(a.U) + at + 4 * (qq & 1);
   };
@@ -197,27 +200,28 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
 
   auto issue = [&](int step, unsigned int to) {
     const int k0 = k_first + step * KSTEP;
-    to += wave * 1024;
+    to += wave * 64 * COPY;
     if (ADAPT && step >= own_steps) {
-#pragma unroll
-      for (int i = 0; i < A::PER; ++i) copy_to_lds(piece_of_u(step, i), to + i * THREADS * 16);
-#pragma unroll
+      // (few steps with long addresses: not unrolled where there are many copies)
+#pragma unroll COPY == 16 ? 4 : 1
+      for (int i = 0; i < A::PER; ++i) copy_to_lds<COPY>(piece_of_u(step, i), to + i * THREADS * COPY);
+#pragma unroll COPY == 16 ? 4 : 1
       for (int i = 0; i < B::PER; ++i) {
         const T* row = row_of_b(step, i);
-        copy_to_lds(row ? static_cast<const void*>(row + min(n0 + B::piece_of(i) * EPC, a.N - EPC)) : &g_zeros, to + A::BYTES + i * THREADS * 16);
+        copy_to_lds<COPY>(row ? static_cast<const void*>(row + min(n0 + B::element_of(i), a.N - E)) : &g_zeros, to + A::BYTES + i * THREADS * COPY);
       }
     } else if (k0 + KSTEP <= k_end) {
 #pragma unroll
-      for (int i = 0; i < A::PER; ++i) copy_to_lds(pa[i] + k0, to + i * THREADS * 16);
+      for (int i = 0; i < A::PER; ++i) copy_to_lds<COPY>(pa[i] + k0, to + i * THREADS * COPY);
 #pragma unroll
-      for (int i = 0; i < B::PER; ++i) copy_to_lds(pb[i] + k0 * step_b, to + A::BYTES + i * THREADS * 16);
+      for (int i = 0; i < B::PER; ++i) copy_to_lds<COPY>(pb[i] + k0 * step_b, to + A::BYTES + i * THREADS * COPY);
     } else {
 #pragma unroll
       for (int i = 0; i < A::PER; ++i)
-        copy_to_lds(k0 + va[i] < k_end ? static_cast<const void*>(pa[i] + k0) : &g_zeros, to + i * THREADS * 16);
+        copy_to_lds<COPY>(k0 + va[i] < k_end ? static_cast<const void*>(pa[i] + k0) : &g_zeros, to + i * THREADS * COPY);
 #pragma unroll
       for (int i = 0; i < B::PER; ++i)
-        copy_to_lds(k0 + vb[i] < k_end ? static_cast<const void*>(pb[i] + k0 * step_b) : &g_zeros, to + A::BYTES + i * THREADS * 16);
+        copy_to_lds<COPY>(k0 + vb[i] < k_end ? static_cast<const void*>(pb[i] + k0 * step_b) : &g_zeros, to + A::BYTES + i * THREADS * COPY);
     }
   };
   // Up to here all 16 bytes of a piece may be read: a row of X ends behind it; a row of W may end inside it, but another follows.
@@ -251,7 +255,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
     }
 #pragma unroll
     for (int i = 0; i < B::PER; ++i) {
-      const int n = n0 + B::piece_of(i) * EPC;
+      const int n = n0 + B::element_of(i);
       u32x4 v;
       if (of_adapters) {
         const T* row = row_of_b(step, i);
@@ -317,18 +321,18 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
   }
 }
 
-template <typename T, class S, bool BT, bool DIRECT, bool ADAPT> int launch(GroupedArgs a, int splits, hipStream_t s) {
+template <typename T, class S, bool BT, int COPY, bool ADAPT> int launch(GroupedArgs a, int splits, hipStream_t s) {
   constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
-  typedef Operand<T, true, S::TM, S::THREADS, KBYTES> A;
-  typedef Operand<T, BT, S::TN, S::THREADS, KBYTES> B;
-  constexpr int LDS = (DIRECT ? S::RING : 2) * (A::BYTES + B::BYTES);
+  typedef Operand<T, true, S::TM, S::THREADS, KBYTES, COPY ? COPY : 16> A;
+  typedef Operand<T, BT, S::TN, S::THREADS, KBYTES, COPY ? COPY : 16> B;
+  constexpr int LDS = (COPY ? S::RING : 2) * (A::BYTES + B::BYTES);
   a.tiles_n = (a.n_store + S::TN - 1) / S::TN;
   a.row_tiles = ADAPT ? (a.n + S::TM - 1) / S::TM : a.n / S::TM + std::min(a.n, a.G + 1);
   const int steps = (a.K + A::KSTEP - 1) / A::KSTEP;
   a.steps_per_split = (steps + splits - 1) / splits;
   const int64_t blocks = static_cast<int64_t>(a.tiles_n) * a.row_tiles;
   if (blocks > 0x7fffffff) return fail(LQ_ERR_UNSUPPORTED, "grouped product: %lld tiles are more than one launch takes", (long long)blocks);
-  const auto kernel = grouped_product_kernel<T, S, BT, DIRECT, ADAPT>;
+  const auto kernel = grouped_product_kernel<T, S, BT, COPY, ADAPT>;
   if (LDS >= 64 * 1024)
     LQ_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
   kernel<<<dim3(static_cast<unsigned>(blocks), splits), S::THREADS, LDS, s>>>(a);
@@ -341,22 +345,30 @@ typedef TileShape<64, 64, 2, 2> Tile64;
 typedef TileShape<64, 64, 2, 2, 4> Tile64Ahead;
 typedef TileShape<256, 256, 2, 4, 4> Tile256;
 
-template <typename T, bool BT, bool DIRECT, bool ADAPT> int by_size(const GroupedArgs& a, int splits, hipStream_t s) {
+template <typename T, bool BT, int COPY, bool ADAPT> int by_size(const GroupedArgs& a, int splits, hipStream_t s) {
   const int64_t large = static_cast<int64_t>((a.n_store + 127) / 128) * ((a.n + 127) / 128);
-  if constexpr (sizeof(T) == 2 && DIRECT)
-    if (large >= 4 * num_cus()) return launch<T, Tile256, BT, DIRECT, ADAPT>(a, splits, s);
-  if (large >= num_cus()) return launch<T, Tile128, BT, DIRECT, ADAPT>(a, splits, s);
+  if constexpr (sizeof(T) == 2 && COPY == 16)
+    if (large >= 4 * num_cus()) return launch<T, Tile256, BT, COPY, ADAPT>(a, splits, s);
+  // (adapters in copies of 4 bytes: the addresses of the larger tile's copies do not fit in the registers beside the rest)
+  if constexpr (!(ADAPT && COPY == 4))
+    if (large >= num_cus()) return launch<T, Tile128, BT, COPY, ADAPT>(a, splits, s);
   // Few tiles: three steps ahead in each instead of several workgroups a compute unit (64 rows, 4,096 -> 4,096 with adapters: 59 -> 44 us;
   // 1,024 tiles of 64 experts' matrices, 2,048 -> 1,024: 45 us three steps ahead, 38 one).
   const int64_t small = static_cast<int64_t>((a.n_store + 63) / 64) * ((a.n + 63) / 64 + (ADAPT ? 0 : std::min(a.n, a.G) / 2)) * splits;
-  if constexpr (DIRECT)
-    if (small < 3 * num_cus()) return launch<T, Tile64Ahead, BT, DIRECT, ADAPT>(a, splits, s);
-  return launch<T, Tile64, BT, DIRECT, ADAPT>(a, splits, s);
+  if constexpr (COPY != 0)
+    if (small < 3 * num_cus()) return launch<T, Tile64Ahead, BT, COPY, ADAPT>(a, splits, s);
+  return launch<T, Tile64, BT, COPY, ADAPT>(a, splits, s);
 }
 
-template <typename T> int product(const GroupedArgs& a, bool transposed, bool in_vec, int splits, hipStream_t s) {
-  if (transposed) return in_vec ? by_size<T, true, true, false>(a, splits, s) : by_size<T, true, false, false>(a, splits, s);
-  return in_vec ? by_size<T, false, true, false>(a, splits, s) : by_size<T, false, false, false>(a, splits, s);
+template <typename T, bool BT, bool ADAPT> int by_copy(const GroupedArgs& a, int copy, int splits, hipStream_t s) {
+  if (copy == 16) return by_size<T, BT, 16, ADAPT>(a, splits, s);
+  if constexpr (sizeof(T) == 2)
+    if (copy == 0) return by_size<T, BT, 0, ADAPT>(a, splits, s);
+  return by_size<T, BT, 4, ADAPT>(a, splits, s);
+}
+
+template <typename T> int product(const GroupedArgs& a, bool transposed, int copy, int splits, hipStream_t s) {
+  return transposed ? by_copy<T, true, false>(a, copy, splits, s) : by_copy<T, false, false>(a, copy, splits, s);
 }
 
 // U from the partial sums of its product: scaled, zeros behind the last rank, as two bf16 numbers beside bf16 matrices.  Eight
@@ -396,14 +408,14 @@ __global__ __launch_bounds__(256) void adapter_scale_kernel(const float* __restr
 
 }  // namespace
 
-int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed, bool in_vec, hipStream_t s) {
-  return dtype == LQ_BF16 ? product<bf16_t>(a, transposed, in_vec, 1, s) : product<float>(a, transposed, in_vec, 1, s);
+int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed, int copy, hipStream_t s) {
+  return dtype == LQ_BF16 ? product<bf16_t>(a, transposed, copy, 1, s) : product<float>(a, transposed, copy, 1, s);
 }
 
-int launch_adapter_product(const GroupedArgs& m, const GroupedArgs& low, int splits, const float* scale, void* u, int32_t dtype, bool main_vec,
-                           bool low_vec, hipStream_t s) {
+int launch_adapter_product(const GroupedArgs& m, const GroupedArgs& low, int splits, const float* scale, void* u, int32_t dtype, int main_copy,
+                           int low_copy, hipStream_t s) {
   const bool halves = dtype == LQ_BF16;
-  const int rc = halves ? product<bf16_t>(low, false, low_vec, splits, s) : product<float>(low, false, low_vec, splits, s);
+  const int rc = halves ? product<bf16_t>(low, false, low_copy, splits, s) : product<float>(low, false, low_copy, splits, s);
   if (rc) return rc;
   const int per = m.rp / 8;
   const int64_t pieces = static_cast<int64_t>(m.n) * per;
@@ -412,8 +424,7 @@ int launch_adapter_product(const GroupedArgs& m, const GroupedArgs& low, int spl
   if (halves) adapter_scale_kernel<true><<<blocks, 256, 0, s>>>(part, splits, low.split_stride, pieces, per, m.rank, scale, low.gpos, u, m.u_rest);
   else adapter_scale_kernel<false><<<blocks, 256, 0, s>>>(part, splits, low.split_stride, pieces, per, m.rank, scale, low.gpos, u, 0);
   LQ_LAUNCH_CHECK("adapter_scale_kernel");
-  if (halves) return main_vec ? by_size<bf16_t, false, true, true>(m, 1, s) : by_size<bf16_t, false, false, true>(m, 1, s);
-  return main_vec ? by_size<float, false, true, true>(m, 1, s) : by_size<float, false, false, true>(m, 1, s);
+  return halves ? by_copy<bf16_t, false, true>(m, main_copy, 1, s) : by_copy<float, false, true>(m, main_copy, 1, s);
 }
 
 }  // namespace lq
