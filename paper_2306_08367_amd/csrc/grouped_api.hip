@@ -78,18 +78,6 @@ int piece_bytes(const lq_stack& w) { return piece_bytes(w.data, w.ld, w.cols, w.
 // Rows that start on 16-byte boundaries.
 bool aligned_rows(const void* data, int64_t ld, int32_t dtype) { return aligned(data, 16) && ld % (16 / static_cast<int64_t>(dtype_size(dtype))) == 0; }
 
-// Splits of the inner dimension of the product that makes U: enough for two workgroups of 64 x 64 a compute unit, and at least
-// four steps each.
-int adapter_splits(int64_t n, int32_t k, int32_t rp, int32_t dtype) {
-  const int64_t tiles = ((n + 63) / 64) * ((rp + 63) / 64);
-  const int64_t steps = (k + 128 / static_cast<int64_t>(dtype_size(dtype)) - 1) / (128 / static_cast<int64_t>(dtype_size(dtype)));
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), steps / 4, 16})));
-}
-
-// Workspace: 256 bytes for LQ_CHECK_FKS, partial sums of U [splits x n x rp] fp32, U [n x rp] (fp32 or two bf16 numbers), the group of
-// every position.
-size_t adapter_u_bytes(int64_t n, int32_t rp, int splits) { return round_up(static_cast<size_t>(splits) * n * rp * 4, 256); }
-
 }  // namespace
 }  // namespace lq
 
@@ -220,8 +208,7 @@ size_t lq_adapter_workspace_bytes(int64_t n, int32_t n_groups, int32_t k, int32_
   if (n < 0 || n > MAX_POSITIONS || n_groups < 1 || n_groups > LQ_MAX_MODELS || k < 1 || l < 1 || rank < 1 || rank > LQ_MAX_RANK ||
       !dtype_ok(dtype))
     return 0;
-  const int32_t rp = (rank + 7) / 8 * 8;
-  return 256 + adapter_u_bytes(n, rp, adapter_splits(n, k, rp, dtype)) + adapter_u_bytes(n, rp, 1) + round_up(static_cast<size_t>(n) * 4, 256);
+  return adapter_ws_bytes(n, k, l, rank, dtype);
 }
 
 int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W, const lq_mat* bias, const lq_stack* A,
@@ -254,26 +241,16 @@ int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W
   if ((rc = verify_groups(*groups, flags, ws, ws_bytes, s))) return rc;
   if (n == 0) return LQ_OK;
 
-  const int32_t rp = (rank + 7) / 8 * 8;
-  const int splits = adapter_splits(n, k, rp, dt);
-  char* part = static_cast<char*>(ws) + 256;
-  char* U = part + adapter_u_bytes(n, rp, splits);
-  int32_t* group_of = reinterpret_cast<int32_t*>(U + adapter_u_bytes(n, rp, 1));
   GroupedArgs a{};
   a.off = groups->offsets; a.order = groups->order; a.G = groups->n_groups; a.n = static_cast<int32_t>(n);
   a.X = X->data; a.ldx = X->ld; a.K = k; a.slots = 1;
-  GroupedArgs low = a;
-  low.W = A->data; low.ldw = A->ld; low.sw = A->stride;
-  low.Y = part; low.ldy = rp; low.N = rank; low.n_store = rp; low.y_grouped = 1; low.y_vec = 1;
-  low.split_stride = n * rp; low.gpos = group_of;
   a.W = W->data; a.ldw = W->ld;
   if (bias) { a.bias = bias->data; a.ldb = bias->ld; }
   a.Y = Y->data; a.ldy = Y->ld; a.y_bf16 = Y->dtype == LQ_BF16; a.N = l; a.n_store = l;
   a.y_vec = aligned_rows(Y->data, Y->ld, Y->dtype) && (!bias || aligned_rows(bias->data, bias->ld, bias->dtype));
-  a.U = U; a.u_rest = n * rp; a.rp = rp; a.rank = rank;
-  a.B = B->data; a.ldB = B->ld; a.sB = B->stride; a.group_of = group_of;
+  a.B = B->data; a.ldB = B->ld; a.sB = B->stride; a.rank = rank;
   const int of_x = piece_bytes(*X);
-  return launch_adapter_product(a, low, splits, scale, U, dt, std::min({of_x, piece_bytes(*W), piece_bytes(*B)}), std::min(of_x, piece_bytes(*A)), s);
+  return launch_adapter_product(a, *A, scale, ws, dt, std::min({of_x, piece_bytes(*W), piece_bytes(*B)}), std::min(of_x, piece_bytes(*A)), s);
 }
 
 }  // extern "C"

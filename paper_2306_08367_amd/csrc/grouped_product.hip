@@ -17,12 +17,12 @@ namespace {
 
 // Bias, ReLU and gate, and the rows m of the tile for which stored(m).
 template <typename T, class S, typename F>
-__device__ __forceinline__ void store_tile(const GroupedArgs& a, const RowTile& tile, int n0, const int* yrow, f32x4 (&acc)[S::MI][S::NI], F&& stored) {
+__device__ __forceinline__ void store_tile(const GroupedArgs& a, const RowTile& tile, int n0, int split, const int* yrow, f32x4 (&acc)[S::MI][S::NI], F&& stored) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = (wave / S::WAVES_N) * S::MI * 16, wn = n0 + (wave % S::WAVES_N) * S::NI * 16;
   const bool has_bias = a.bias && tile.group >= 0;
   const T* bias = static_cast<const T*>(a.bias) + (has_bias ? tile.group * a.ldb : 0);
-  char* const Y = static_cast<char*>(a.Y) + blockIdx.y * a.split_stride * (a.y_bf16 ? 2 : 4);
+  char* const Y = static_cast<char*>(a.Y) + split * a.split_stride * (a.y_bf16 ? 2 : 4);
   if (S::NI == 4 && a.y_vec && wn + 64 <= a.n_store && wn + 64 <= a.N) {
     // 16 neighbouring columns of a row a lane
     const int n = wn + 16 * (lane >> 4);
@@ -96,8 +96,9 @@ __device__ __forceinline__ void store_tile(const GroupedArgs& a, const RowTile& 
   }
 }
 
+// Workgroup `block` of the product's grid, split `split` of its inner dimension.
 template <typename T, class S, bool BT, int COPY, bool ADAPT>
-__global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedArgs a) {
+__device__ __forceinline__ void tile_product(const GroupedArgs& a, int block, int split) {
   constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
   typedef Operand<T, true, S::TM, S::THREADS, KBYTES, COPY ? COPY : 16> A;
   typedef Operand<T, BT, S::TN, S::THREADS, KBYTES, COPY ? COPY : 16> B;
@@ -109,8 +110,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   RowTile tile;
-  if constexpr (ADAPT) tile = all_rows<S::TM>(a.n, blockIdx.x, a.tiles_n);
-  else tile = find_tile<S::TM>(a.off, a.G, a.n, blockIdx.x, a.tiles_n);
+  if (ADAPT || !a.off) tile = all_rows<S::TM>(a.n, block, a.tiles_n);
+  else tile = find_tile<S::TM>(a.off, a.G, a.n, block, a.tiles_n);
   const int n0 = tile.col * S::TN;
   if (tile.rows <= 0) return;
 
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
     const int r = a.order ? a.order[p] : p;
     xrow[m] = a.x_grouped ? p : r / a.slots;
     yrow[m] = a.y_grouped ? p : r;
-    if (!ADAPT && a.gpos && in && n0 == 0 && blockIdx.y == 0) a.gpos[p] = tile.group;
+    if (!ADAPT && a.gpos && in && n0 == 0 && split == 0) a.gpos[p] = tile.group;
   }
   __syncthreads();
 
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
     __syncthreads();
   }
 
-  const int k_first = blockIdx.y * a.steps_per_split * KSTEP;
+  const int k_first = split * a.steps_per_split * KSTEP;
   const int k_end = min(a.K, k_first + a.steps_per_split * KSTEP);
   const bool any = tile.group >= 0 && k_first < k_end;
   const T* X = static_cast<const T*>(a.X);
@@ -294,7 +295,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
       }
     }
     if constexpr (!ADAPT) {
-      store_tile<T, S>(a, tile, n0, yrow, acc, [](int) { return true; });
+      store_tile<T, S>(a, tile, n0, split, yrow, acc, [](int) { return true; });
       return;
     } else {
       // An infinity or a NaN in one adapter's B, times the zeros in the rows of others, is a NaN there.  A tile with a NaN
@@ -309,11 +310,11 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
 #pragma unroll
             for (int q = 0; q < 4; ++q) nan |= acc[i][j][q] != acc[i][j][q];
         if (!__syncthreads_or(nan)) {
-          store_tile<T, S>(a, tile, n0, yrow, acc, [](int) { return true; });
+          store_tile<T, S>(a, tile, n0, split, yrow, acc, [](int) { return true; });
           return;
         }
       } else {
-        store_tile<T, S>(a, tile, n0, yrow, acc, [&](int m) { return which[m] == (only < adapters ? only : -1); });
+        store_tile<T, S>(a, tile, n0, split, yrow, acc, [&](int m) { return which[m] == (only < adapters ? only : -1); });
         __syncthreads();           // (LDS is read to its end)
       }
       if (++only > adapters) return;
@@ -321,15 +322,33 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedA
   }
 }
 
+template <typename T, class S, bool BT, int COPY, bool ADAPT>
+__global__ __launch_bounds__(S::THREADS, 2) void grouped_product_kernel(GroupedArgs a) {
+  tile_product<T, S, BT, COPY, ADAPT>(a, blockIdx.x, blockIdx.y);
+}
+
+// Two products in one launch: the first `blocks_a` workgroups work on a, `splits` after `splits`, the others on b.
+template <typename T, class S, int COPY>
+__global__ __launch_bounds__(S::THREADS, 2) void grouped_pair_kernel(GroupedArgs a, GroupedArgs b, int blocks_a) {
+  const bool first = static_cast<int>(blockIdx.x) < blocks_a;
+  const GroupedArgs& g = first ? a : b;
+  const int at = blockIdx.x - (first ? 0 : blocks_a), tiles = g.tiles_n * g.row_tiles;
+  tile_product<T, S, false, COPY, false>(g, at % tiles, at / tiles);
+}
+
+// `one`: all positions use one matrix (else there can be a part of a tile more for every group).
+void set_tiles(GroupedArgs& a, int tm, int tn, int step, bool one, int splits) {
+  a.tiles_n = (a.n_store + tn - 1) / tn;
+  a.row_tiles = one ? (a.n + tm - 1) / tm : a.n / tm + std::min(a.n, a.G + 1);
+  a.steps_per_split = ((a.K + step - 1) / step + splits - 1) / splits;
+}
+
 template <typename T, class S, bool BT, int COPY, bool ADAPT> int launch(GroupedArgs a, int splits, hipStream_t s) {
   constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
   typedef Operand<T, true, S::TM, S::THREADS, KBYTES, COPY ? COPY : 16> A;
   typedef Operand<T, BT, S::TN, S::THREADS, KBYTES, COPY ? COPY : 16> B;
   constexpr int LDS = (COPY ? S::RING : 2) * (A::BYTES + B::BYTES);
-  a.tiles_n = (a.n_store + S::TN - 1) / S::TN;
-  a.row_tiles = ADAPT ? (a.n + S::TM - 1) / S::TM : a.n / S::TM + std::min(a.n, a.G + 1);
-  const int steps = (a.K + A::KSTEP - 1) / A::KSTEP;
-  a.steps_per_split = (steps + splits - 1) / splits;
+  set_tiles(a, S::TM, S::TN, A::KSTEP, ADAPT, splits);
   const int64_t blocks = static_cast<int64_t>(a.tiles_n) * a.row_tiles;
   if (blocks > 0x7fffffff) return fail(LQ_ERR_UNSUPPORTED, "grouped product: %lld tiles are more than one launch takes", (long long)blocks);
   const auto kernel = grouped_product_kernel<T, S, BT, COPY, ADAPT>;
@@ -356,7 +375,7 @@ template <typename T, bool BT, int COPY, bool ADAPT> int by_size(const GroupedAr
   // 1,024 tiles of 64 experts' matrices, 2,048 -> 1,024: 45 us three steps ahead, 38 one).
   const int64_t small = static_cast<int64_t>((a.n_store + 63) / 64) * ((a.n + 63) / 64 + (ADAPT ? 0 : std::min(a.n, a.G) / 2)) * splits;
   if constexpr (COPY != 0)
-    if (small < 3 * num_cus()) return launch<T, Tile64Ahead, BT, COPY, ADAPT>(a, splits, s);
+    if (small <= 2 * num_cus()) return launch<T, Tile64Ahead, BT, COPY, ADAPT>(a, splits, s);
   return launch<T, Tile64, BT, COPY, ADAPT>(a, splits, s);
 }
 
@@ -406,23 +425,140 @@ __global__ __launch_bounds__(256) void adapter_scale_kernel(const float* __restr
   }
 }
 
+// Few rows: partial sums of X W [splits x n x l] and of U, added up here, with U B in fp32: one row and 1,024 columns a
+// workgroup.
+template <typename T>
+__global__ __launch_bounds__(256) void adapter_finish_kernel(GroupedArgs a, const float* __restrict__ sums, int splits, const float* __restrict__ part,
+                                                             int u_splits, const float* __restrict__ scale) {
+  __shared__ float u[LQ_MAX_RANK];
+  const int p = blockIdx.x, g = a.group_of[p], r = a.order ? a.order[p] : p;
+  const float s = g >= 0 && scale ? scale[g] : 1.f;
+  if (g >= 0 && static_cast<int>(threadIdx.x) < a.rank) {
+    float v = 0.f;
+    for (int z = 0; z < u_splits; ++z) v += part[(static_cast<int64_t>(z) * a.n + p) * a.rp + threadIdx.x];
+    u[threadIdx.x] = v * s;
+  }
+  __syncthreads();
+  const int n = blockIdx.y * 1024 + 4 * threadIdx.x, valid = a.N - n;
+  if (valid <= 0) return;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  for (int z = 0; z < splits; ++z) y += load_four(sums + (static_cast<int64_t>(z) * a.n + p) * a.n_store + n, valid);
+  if (g >= 0) {
+    const T* B = static_cast<const T*>(a.B) + g * a.sB + n;
+    f32x4 low = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int k = 0; k < a.rank; ++k) low += u[k] * load_four(B + k * a.ldB, valid);
+    y += low;
+  }
+  if (a.bias) y += load_four(static_cast<const T*>(a.bias) + n, valid);
+  if (a.y_bf16) store_four<true>(a.Y, static_cast<int64_t>(r) * a.ldy + n, valid, y);
+  else store_four<false>(a.Y, static_cast<int64_t>(r) * a.ldy + n, valid, y);
+}
+
+// How an adapter product runs, and what lies where in its workspace behind the first 256 bytes (kept for LQ_CHECK_FKS).
+//   few rows    the products of X with W and with A in one launch of tiles of 64 x 64, both in splits of the inner dimension so that
+//               there are two tiles a compute unit, then adapter_finish_kernel: where W alone has at most one tile a compute unit and
+//               the rows' own reads of B (every row reads its adapter) stay small against the caches.  64 rows of 4,096 -> 4,096 with 48
+//               adapters: 44 us in tiles
+//   else        U first, then one product (tile_product, ADAPT)
+struct AdapterPlan {
+  bool few;
+  int rp, splits, u_splits;
+  size_t part, u, group_of, sums, bytes;
+};
+AdapterPlan adapter_plan(int64_t n, int32_t k, int32_t l, int32_t rank, int32_t dtype) {
+  AdapterPlan p{};
+  const int64_t size = static_cast<int64_t>(dtype_size(dtype)), steps = (k * size + 127) / 128, cus = 256;
+  p.rp = (rank + 7) / 8 * 8;
+  auto splits = [&](int64_t columns, int64_t wanted) {      // at least four steps each
+    const int64_t tiles = std::max<int64_t>((n + 63) / 64 * ((columns + 63) / 64), 1);
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({wanted / tiles, steps / 4, 16})));
+  };
+  p.few = (n + 63) / 64 * ((l + 63) / 64) <= cus && n * rank * l * size <= (32ll << 20);
+  p.u_splits = splits(p.rp, 2 * cus);
+  p.splits = p.few ? splits(l, 2 * cus) : 1;
+  p.part = 256;
+  p.u = p.part + round_up(static_cast<size_t>(p.u_splits) * n * p.rp * 4, 256);
+  p.group_of = p.u + (p.few ? 0 : round_up(static_cast<size_t>(n) * p.rp * 4, 256));
+  p.sums = p.group_of + round_up(static_cast<size_t>(n) * 4, 256);
+  p.bytes = p.sums + (p.few ? round_up(static_cast<size_t>(p.splits) * n * l * 4, 256) : 0);
+  return p;
+}
+
+template <typename T, int COPY> int launch_pair(GroupedArgs a, GroupedArgs b, int splits_a, int splits_b, hipStream_t s) {
+  typedef TileShape<64, 64, 2, 2, 4> S;
+  typedef Operand<T, true, S::TM, S::THREADS, 128, COPY ? COPY : 16> A;
+  constexpr int LDS = (COPY ? S::RING : 2) * 2 * A::BYTES;
+  set_tiles(a, S::TM, S::TN, A::KSTEP, true, splits_a);
+  set_tiles(b, S::TM, S::TN, A::KSTEP, false, splits_b);
+  const int blocks_a = a.tiles_n * a.row_tiles * splits_a, blocks_b = b.tiles_n * b.row_tiles * splits_b;
+  const auto kernel = grouped_pair_kernel<T, S, COPY>;
+  if (LDS >= 64 * 1024)
+    LQ_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+  kernel<<<blocks_a + blocks_b, S::THREADS, LDS, s>>>(a, b, blocks_a);
+  LQ_LAUNCH_CHECK("grouped_pair_kernel");
+  return LQ_OK;
+}
+
+template <typename T> int few_rows(const GroupedArgs& m, GroupedArgs low, const AdapterPlan& p, const float* scale, char* ws, int copy, hipStream_t s) {
+  GroupedArgs a = m;
+  a.off = nullptr;
+  a.bias = nullptr;
+  a.Y = ws + p.sums;
+  a.ldy = a.n_store;
+  a.split_stride = static_cast<int64_t>(a.n) * a.n_store;
+  a.y_grouped = 1;
+  a.y_bf16 = 0;
+  a.y_vec = a.n_store % 4 == 0;
+  int rc;
+  if (copy == 16) rc = launch_pair<T, 16>(a, low, p.splits, p.u_splits, s);
+  else if (sizeof(T) == 4 || copy == 4) rc = launch_pair<T, 4>(a, low, p.splits, p.u_splits, s);
+  else rc = launch_pair<T, sizeof(T) == 4 ? 4 : 0>(a, low, p.splits, p.u_splits, s);
+  if (rc) return rc;
+  adapter_finish_kernel<T><<<dim3(m.n, (m.N + 1023) / 1024), 256, 0, s>>>(m, static_cast<const float*>(a.Y), p.splits, static_cast<const float*>(low.Y),
+                                                                          p.u_splits, scale);
+  LQ_LAUNCH_CHECK("adapter_finish_kernel");
+  return LQ_OK;
+}
+
 }  // namespace
 
 int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed, int copy, hipStream_t s) {
   return dtype == LQ_BF16 ? product<bf16_t>(a, transposed, copy, 1, s) : product<float>(a, transposed, copy, 1, s);
 }
 
-int launch_adapter_product(const GroupedArgs& m, const GroupedArgs& low, int splits, const float* scale, void* u, int32_t dtype, int main_copy,
-                           int low_copy, hipStream_t s) {
+size_t adapter_ws_bytes(int64_t n, int32_t k, int32_t l, int32_t rank, int32_t dtype) { return adapter_plan(n, k, l, rank, dtype).bytes; }
+
+int launch_adapter_product(const GroupedArgs& args, const lq_stack& A, const float* scale, void* ws, int32_t dtype, int main_copy, int low_copy,
+                           hipStream_t s) {
+  GroupedArgs m = args;
+  const AdapterPlan p = adapter_plan(m.n, m.K, m.N, m.rank, dtype);
+  char* const base = static_cast<char*>(ws);
+  m.rp = p.rp;
+  m.u_rest = static_cast<int64_t>(m.n) * p.rp;
+  m.U = base + p.u;
+  m.group_of = reinterpret_cast<const int32_t*>(base + p.group_of);
+  GroupedArgs low{};
+  low.off = m.off; low.order = m.order; low.G = m.G; low.n = m.n;
+  low.X = m.X; low.ldx = m.ldx; low.K = m.K; low.slots = 1;
+  low.W = A.data; low.ldw = A.ld; low.sw = A.stride;
+  low.Y = base + p.part; low.ldy = p.rp; low.N = m.rank; low.n_store = p.rp; low.y_grouped = 1; low.y_vec = 1;
+  low.split_stride = static_cast<int64_t>(m.n) * p.rp;
+  low.gpos = reinterpret_cast<int32_t*>(base + p.group_of);
   const bool halves = dtype == LQ_BF16;
-  const int rc = halves ? product<bf16_t>(low, false, low_copy, splits, s) : product<float>(low, false, low_copy, splits, s);
+  if (p.few) {
+    const int copy = std::min(main_copy, low_copy);
+    return halves ? few_rows<bf16_t>(m, low, p, scale, base, copy, s) : few_rows<float>(m, low, p, scale, base, copy, s);
+  }
+  const int rc = halves ? product<bf16_t>(low, false, low_copy, p.u_splits, s) : product<float>(low, false, low_copy, p.u_splits, s);
   if (rc) return rc;
   const int per = m.rp / 8;
   const int64_t pieces = static_cast<int64_t>(m.n) * per;
   const unsigned blocks = static_cast<unsigned>((pieces + 255) / 256);
   const float* part = static_cast<const float*>(low.Y);
-  if (halves) adapter_scale_kernel<true><<<blocks, 256, 0, s>>>(part, splits, low.split_stride, pieces, per, m.rank, scale, low.gpos, u, m.u_rest);
-  else adapter_scale_kernel<false><<<blocks, 256, 0, s>>>(part, splits, low.split_stride, pieces, per, m.rank, scale, low.gpos, u, 0);
+  void* u = base + p.u;
+  if (halves) adapter_scale_kernel<true><<<blocks, 256, 0, s>>>(part, p.u_splits, low.split_stride, pieces, per, m.rank, scale, low.gpos, u, m.u_rest);
+  else adapter_scale_kernel<false><<<blocks, 256, 0, s>>>(part, p.u_splits, low.split_stride, pieces, per, m.rank, scale, low.gpos, u, 0);
   LQ_LAUNCH_CHECK("adapter_scale_kernel");
   return halves ? by_copy<bf16_t, false, true>(m, main_copy, 1, s) : by_copy<float, false, true>(m, main_copy, 1, s);
 }
