@@ -208,7 +208,7 @@ size_t lq_adapter_workspace_bytes(int64_t n, int32_t n_groups, int32_t k, int32_
   if (n < 0 || n > MAX_POSITIONS || n_groups < 1 || n_groups > LQ_MAX_MODELS || k < 1 || l < 1 || rank < 1 || rank > LQ_MAX_RANK ||
       !dtype_ok(dtype))
     return 0;
-  return adapter_ws_bytes(n, k, l, rank, dtype);
+  return adapter_ws_bytes(n, n_groups, k, l, rank, dtype);
 }
 
 int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W, const lq_mat* bias, const lq_stack* A,

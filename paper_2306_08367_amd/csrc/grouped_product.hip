@@ -431,23 +431,40 @@ template <typename T>
 __global__ __launch_bounds__(256) void adapter_finish_kernel(GroupedArgs a, const float* __restrict__ sums, int splits, const float* __restrict__ part,
                                                              int u_splits, const float* __restrict__ scale) {
   __shared__ float u[LQ_MAX_RANK];
+  constexpr int AHEAD = 8;
   const int p = blockIdx.x, g = a.group_of[p], r = a.order ? a.order[p] : p;
-  const float s = g >= 0 && scale ? scale[g] : 1.f;
+  const int n = blockIdx.y * 1024 + 4 * threadIdx.x, valid = a.N - n, at = min(n, a.N - 1), there = min(max(valid, 1), 4);
+  // the first partial sums and rows of B are under way while U is added up
+  const float* sum = sums + static_cast<int64_t>(p) * a.n_store + at;
+  const int64_t stride = static_cast<int64_t>(a.n) * a.n_store;
+  const T* B = static_cast<const T*>(a.B) + max(g, 0) * a.sB + at;
+  f32x4 part_y[AHEAD], row[AHEAD];
+#pragma unroll
+  for (int z = 0; z < AHEAD; ++z) part_y[z] = load_four(sum + min(z, splits - 1) * stride, there);
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) row[k] = load_four(B + min(k, a.rank - 1) * a.ldB, there);
   if (g >= 0 && static_cast<int>(threadIdx.x) < a.rank) {
+    const float* of = part + static_cast<int64_t>(p) * a.rp + threadIdx.x;
+    const int64_t step = static_cast<int64_t>(a.n) * a.rp;
     float v = 0.f;
-    for (int z = 0; z < u_splits; ++z) v += part[(static_cast<int64_t>(z) * a.n + p) * a.rp + threadIdx.x];
-    u[threadIdx.x] = v * s;
+#pragma unroll 8
+    for (int z = 0; z < u_splits; ++z) v += of[z * step];
+    u[threadIdx.x] = scale ? v * scale[g] : v;
   }
   __syncthreads();
-  const int n = blockIdx.y * 1024 + 4 * threadIdx.x, valid = a.N - n;
   if (valid <= 0) return;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  for (int z = 0; z < splits; ++z) y += load_four(sums + (static_cast<int64_t>(z) * a.n + p) * a.n_store + n, valid);
+#pragma unroll
+  for (int z = 0; z < AHEAD; ++z)
+    if (z < splits) y += part_y[z];
+  for (int z = AHEAD; z < splits; ++z) y += load_four(sum + z * stride, valid);
   if (g >= 0) {
-    const T* B = static_cast<const T*>(a.B) + g * a.sB + n;
     f32x4 low = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (k < a.rank) low += u[k] * row[k];
 #pragma unroll 8
-    for (int k = 0; k < a.rank; ++k) low += u[k] * load_four(B + k * a.ldB, valid);
+    for (int k = AHEAD; k < a.rank; ++k) low += u[k] * load_four(B + k * a.ldB, valid);
     y += low;
   }
   if (a.bias) y += load_four(static_cast<const T*>(a.bias) + n, valid);
@@ -466,17 +483,17 @@ struct AdapterPlan {
   int rp, splits, u_splits;
   size_t part, u, group_of, sums, bytes;
 };
-AdapterPlan adapter_plan(int64_t n, int32_t k, int32_t l, int32_t rank, int32_t dtype) {
+AdapterPlan adapter_plan(int64_t n, int32_t G, int32_t k, int32_t l, int32_t rank, int32_t dtype) {
   AdapterPlan p{};
   const int64_t size = static_cast<int64_t>(dtype_size(dtype)), steps = (k * size + 127) / 128, cus = 256;
   p.rp = (rank + 7) / 8 * 8;
-  auto splits = [&](int64_t columns, int64_t wanted) {      // at least four steps each
-    const int64_t tiles = std::max<int64_t>((n + 63) / 64 * ((columns + 63) / 64), 1);
-    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({wanted / tiles, steps / 4, 16})));
+  auto splits = [&](int64_t rows, int64_t columns, int64_t least) {      // two tiles a compute unit, `least` steps each
+    const int64_t tiles = std::max<int64_t>(rows * ((columns + 63) / 64), 1);
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({2 * cus / tiles, steps / least, 16})));
   };
   p.few = (n + 63) / 64 * ((l + 63) / 64) <= cus && n * rank * l * size <= (32ll << 20);
-  p.u_splits = splits(p.rp, 2 * cus);
-  p.splits = p.few ? splits(l, 2 * cus) : 1;
+  p.u_splits = splits(n / 64 + (p.few ? std::min<int64_t>(n, G) : 1), p.rp, p.few ? 8 : 4);
+  p.splits = p.few ? splits((n + 63) / 64, l, 4) : 1;
   p.part = 256;
   p.u = p.part + round_up(static_cast<size_t>(p.u_splits) * n * p.rp * 4, 256);
   p.group_of = p.u + (p.few ? 0 : round_up(static_cast<size_t>(n) * p.rp * 4, 256));
@@ -486,7 +503,7 @@ AdapterPlan adapter_plan(int64_t n, int32_t k, int32_t l, int32_t rank, int32_t 
 }
 
 template <typename T, int COPY> int launch_pair(GroupedArgs a, GroupedArgs b, int splits_a, int splits_b, hipStream_t s) {
-  typedef TileShape<64, 64, 2, 2, 4> S;
+  typedef TileShape<64, 64, 2, 2, 3> S;
   typedef Operand<T, true, S::TM, S::THREADS, 128, COPY ? COPY : 16> A;
   constexpr int LDS = (COPY ? S::RING : 2) * 2 * A::BYTES;
   set_tiles(a, S::TM, S::TN, A::KSTEP, true, splits_a);
@@ -527,12 +544,12 @@ int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed,
   return dtype == LQ_BF16 ? product<bf16_t>(a, transposed, copy, 1, s) : product<float>(a, transposed, copy, 1, s);
 }
 
-size_t adapter_ws_bytes(int64_t n, int32_t k, int32_t l, int32_t rank, int32_t dtype) { return adapter_plan(n, k, l, rank, dtype).bytes; }
+size_t adapter_ws_bytes(int64_t n, int32_t G, int32_t k, int32_t l, int32_t rank, int32_t dtype) { return adapter_plan(n, G, k, l, rank, dtype).bytes; }
 
 int launch_adapter_product(const GroupedArgs& args, const lq_stack& A, const float* scale, void* ws, int32_t dtype, int main_copy, int low_copy,
                            hipStream_t s) {
   GroupedArgs m = args;
-  const AdapterPlan p = adapter_plan(m.n, m.K, m.N, m.rank, dtype);
+  const AdapterPlan p = adapter_plan(m.n, m.G, m.K, m.N, m.rank, dtype);
   char* const base = static_cast<char*>(ws);
   m.rp = p.rp;
   m.u_rest = static_cast<int64_t>(m.n) * p.rp;
