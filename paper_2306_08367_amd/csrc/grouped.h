@@ -299,9 +299,10 @@ template <typename T, bool KMAJ, int EXT, int THREADS, int KBYTES = 128, int COP
     else return 2 * (((line >> 1) & 1) | ((line >> 2) & 2));
   }
   // The line of the thread's i-th copy, and the element of it that it begins with.
-  static __device__ __forceinline__ int line_of(int i) { return (i * THREADS + static_cast<int>(threadIdx.x)) / (CPL * CPP); }
+  static __device__ __forceinline__ int id_of(int i) { return i * THREADS + static_cast<int>(threadIdx.x % THREADS); }
+  static __device__ __forceinline__ int line_of(int i) { return id_of(i) / (CPL * CPP); }
   static __device__ __forceinline__ int element_of(int i) {
-    const int id = i * THREADS + threadIdx.x, at = id % (CPL * CPP);
+    const int id = id_of(i), at = id % (CPL * CPP);
     return ((at / CPP) ^ spread(id / (CPL * CPP))) * EPC + at % CPP * (COPY / static_cast<int>(sizeof(T)));
   }
   static __device__ __forceinline__ int place(int line, int piece) { return (line * CPL + (piece ^ spread(line))) * 16; }
@@ -412,64 +413,67 @@ __device__ __forceinline__ void multiply_steps(char* lds, int steps, F&& issue, 
   }
 }
 
-// The product of a tile of 8 wavefronts, two on a SIMD, over `units` blocks of 32 inner indexes: issue(u, LDS address) copies
-// block u's operands to LDS, in COPIES instructions a wavefront.  The two wavefronts of a SIMD take turns: while one
-// multiplies a block (32 matrix instructions, 512 clocks), the other one reads its operands of its next block from LDS, so
-// that neither the matrix cores nor LDS wait for the other.  The second four wavefronts run one turn behind the
-// first four, by one barrier more at the start.  In turns: the first four read block u in turn 2 u and multiply it
-// in turn 2 u + 1, the second four one later.  LDS holds four blocks.  Block u + 3 takes the place of block u - 1, whose
-// last readers are the second four in turn 2 u - 1: each wavefront issues its copies for it in the turn in which it reads block u,
-// and waits for its copies of block u + 1 at the end of turn 2 u + 1, with those of two blocks still in flight: they have
-// five or six turns to arrive.
+// The product of a tile of 8 wavefronts, two on a SIMD, over `units` units of 64 inner indexes, each two blocks of 32: issue(block,
+// LDS address) copies a block's operands to LDS, by four wavefronts.  The two wavefronts of a SIMD take turns: one multiplies a
+// unit (64 matrix instructions, 1,024 clocks), reading the operands of the second block while it multiplies the first
+// one; the other one meanwhile reads its operands of the first block of its next unit and issues copies, so that the matrix
+// cores do not wait for LDS or for the way to it.  The second four wavefronts run one turn behind the first four, by one
+// barrier more at the start.  In turns: the first four read unit w in turn 2 w and multiply it in turn 2 w + 1, the second
+// four one later.  LDS holds four blocks.  The first blocks of units are copied by the first four, the second blocks by the
+// second four: block 2 w + 2 in turn 2 w, when everyone has read block 2 w - 2, and block 2 w + 3 in turn 2 w + 1, when everyone
+// has read block 2 w - 1; each is waited for at the end of the next turn, a turn before its first reader.
+// (Turns of one block, 512 clocks: 1,296 TFLOP/s at 8,192^3; the copies, 64 bytes a clock for the whole compute unit, in front of
+// the reads instead of behind them: 1,198.)
 // with_b(b): called with the wavefront's operands of B beside the products.
 template <typename T, class S, class A, class B, typename F, typename H>
 __device__ __forceinline__ void multiply_in_turns(char* lds, int units, F&& issue, f32x4 (&acc)[S::MI][S::NI], H&& with_b) {
-  static_assert(S::THREADS == 512 && S::WAVES_N == 4, "two wavefronts a SIMD");
-  constexpr int BLOCK = A::BYTES + B::BYTES, COPIES = A::PER + B::PER;
-  static_assert(COPIES == 4, "the waits below count copies");
+  static_assert(S::THREADS == 512 && S::WAVES_N == 4 && S::MI == 8 && S::NI == 4, "two wavefronts a SIMD");
+  constexpr int BLOCK = A::BYTES + B::BYTES;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool second = wave >= 4;
   const int m0 = (wave / S::WAVES_N) * S::MI * 16, n0 = (wave % S::WAVES_N) * S::NI * 16;
   const unsigned int at = lds_address(lds);
-  auto turn = [&]() {
+  auto turn = [&](bool copies) {
     fence();
+    if (copies) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     fence();
   };
-  // (the copies of the two youngest blocks may be in flight; at the end there are no younger ones)
-  auto wait_copies = [&](bool younger) {
-    fence();
-    if (younger) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  };
-  for (int u = 0; u < min(units, 3); ++u) issue(u, at + u * BLOCK);
-  wait_copies(units >= 3);
-  turn();
-  if (second) turn();
-  for (int u = 0; u < units; ++u) {
-    const char* from = lds + (u & 3) * BLOCK;
-    u32x4 a[S::MI], b[S::NI];
+  issue(second ? 1 : 0, at + (second ? BLOCK : 0));
+  turn(true);
+  if (second) turn(false);
+  for (int w = 0; w < units; ++w) {
+    const char* from = lds + (w & 1) * 2 * BLOCK;
+    u32x4 a[S::MI], b[2][S::NI];
 #pragma unroll
-    for (int j = 0; j < S::NI; ++j) b[j] = B::fragment(from + A::BYTES, n0 + 16 * j, 0);
+    for (int j = 0; j < S::NI; ++j) b[0][j] = B::fragment(from + A::BYTES, n0 + 16 * j, 0);
 #pragma unroll
     for (int i = 0; i < S::MI; ++i) a[i] = A::fragment(from, m0 + 16 * i, 0);
-    // (the copies, 64 bytes a clock for the whole compute unit, behind the reads: in front of them they kept the reads waiting,
-    // 1,198 against 1,296 TFLOP/s at 8,192^3)
     fence();
-    if (u + 3 < units) issue(u + 3, at + ((u + 3) & 3) * BLOCK);
-    if (second) wait_copies(u + 3 < units);
-    turn();
+    if (w + 1 < units) issue(2 * w + (second ? 3 : 2), at + (((w + 1) & 1) * 2 + (second ? 1 : 0)) * BLOCK);
+    turn(false);
     __builtin_amdgcn_s_setprio(1);
-    with_b(b);
+    from += BLOCK;
+#pragma unroll
+    for (int j = 0; j < S::NI; ++j) b[1][j] = B::fragment(from + A::BYTES, n0 + 16 * j, 0);
+    with_b(b[0]);
+    fence();
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) {
+#pragma unroll
+      for (int j = 0; j < S::NI; ++j) acc[i][j] = multiply<T>(b[0][j], a[i], acc[i][j]);
+      a[i] = A::fragment(from, m0 + 16 * i, 0);
+      fence();     // (the reads stay where they are)
+    }
+    with_b(b[1]);
 #pragma unroll
     for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-      for (int j = 0; j < S::NI; ++j) acc[i][j] = multiply<T>(b[j], a[i], acc[i][j]);
+      for (int j = 0; j < S::NI; ++j) acc[i][j] = multiply<T>(b[1][j], a[i], acc[i][j]);
     __builtin_amdgcn_s_setprio(0);
-    if (!second) wait_copies(u + 3 < units);
-    turn();
+    turn(true);
   }
-  if (!second) turn();
+  if (!second) turn(false);
 }
 
 // Four by four exchange of registers and groups of 16 lanes: register j of lanes 16 g .. 16 g + 15 and register g of lanes 16 j .. .

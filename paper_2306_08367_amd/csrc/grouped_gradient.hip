@@ -19,9 +19,9 @@ constexpr int RUN = 32;           // most tiles of a chunk that go to one die to
 
 template <typename T, class S, int COPY>
 __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(GradientArgs a) {
-  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
-  typedef Operand<T, false, S::TM, S::THREADS, KBYTES, COPY ? COPY : 16> A;
-  typedef Operand<T, false, S::TN, S::THREADS, KBYTES, COPY ? COPY : 16> B;
+  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128, COPIERS = 256;     // threads that copy a step
+  typedef Operand<T, false, S::TM, COPIERS, KBYTES, COPY ? COPY : 16> A;
+  typedef Operand<T, false, S::TN, COPIERS, KBYTES, COPY ? COPY : 16> B;
   constexpr bool DIRECT = COPY != 0;           // through LDS without registers
   constexpr int E = DIRECT ? COPY / static_cast<int>(sizeof(T)) : 1;
   constexpr int KSTEP = A::KSTEP, EPC = A::EPC, THREADS = S::THREADS, BUFFER = A::BYTES + B::BYTES;
@@ -73,11 +73,10 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(Gradien
       yrow[i] = a.y_grouped ? p : r;
     }
     __syncthreads();
-    // Where the pieces of a step lie (rows behind the last one: zeros in both operands).  Row numbers are read from LDS together
-    // with operands and made addresses beside the products, a block ahead of their copies.
+    // Copies of a step (rows behind the last one: zeros in both operands).  With turns, row numbers are read from LDS a turn ahead of
+    // their copies.
     constexpr int COPIES = A::PER + B::PER;
-    const void* from[COPIES];
-    int number[COPIES], ready = -1, looked = -1;
+    int number[COPIES], looked = -1;
     auto look_up = [&](int step) {
 #pragma unroll
       for (int c = 0; c < COPIES; ++c) {
@@ -86,29 +85,19 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_gradient_kernel(Gradien
       }
       looked = step;
     };
-    auto locate = [&]() {
+    auto issue = [&](int step, unsigned int to) {
+      if (THREADS != 512 || looked != step) look_up(step);
 #pragma unroll
       for (int c = 0; c < COPIES; ++c) {
         const T* p = c >= A::PER ? dY + number[c] * a.ldy + cb[c - A::PER] : X + number[c] * a.ldx + ca[c];
-        from[c] = number[c] >= 0 ? static_cast<const void*>(p) : &g_zeros;
+        copy_to_lds<COPY>(number[c] >= 0 ? static_cast<const void*>(p) : &g_zeros,
+                          to + (wave & 3) * 64 * COPY + (c >= A::PER ? A::BYTES + (c - A::PER) * COPIERS * COPY : c * COPIERS * COPY));
       }
-      ready = looked;
-    };
-    auto issue = [&](int step, unsigned int to) {
-      if (ready != step) {
-        look_up(step);
-        locate();
-      }
-#pragma unroll
-      for (int c = 0; c < COPIES; ++c)
-        copy_to_lds<COPY>(from[c], to + wave * 64 * COPY + (c >= A::PER ? A::BYTES + (c - A::PER) * THREADS * COPY : c * THREADS * COPY));
-      if constexpr (THREADS == 512) look_up(step + 1);
+      if constexpr (THREADS == 512) look_up(step + 2);     // (this wavefront's next block)
     };
     if constexpr (DIRECT && THREADS == 512) {
-      multiply_in_turns<T, S, A, B>(lds, steps, issue, acc, [&](const u32x4(&b)[S::NI]) {
-        add_up(b);
-        locate();
-      });
+      // (a block behind the last one is zeros)
+      multiply_in_turns<T, S, A, B>(lds, (steps + 1) >> 1, issue, acc, add_up);
     } else if constexpr (DIRECT) {
       multiply_steps<T, S, A, B, S::RING>(lds, steps, issue, acc, [&](const u32x4(&b)[S::NI]) { add_up(b); });
     } else {
@@ -281,9 +270,9 @@ Plan plan_of(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype, int copy
 size_t place_bytes(int64_t places, int32_t k, int32_t l) { return static_cast<size_t>(places) * (static_cast<size_t>(k) + 1) * l * 4; }
 
 template <typename T, class S, int COPY> int launch(GradientArgs a, const Plan& p, hipStream_t s) {
-  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
-  typedef Operand<T, false, S::TM, S::THREADS, KBYTES, COPY ? COPY : 16> A;
-  typedef Operand<T, false, S::TN, S::THREADS, KBYTES, COPY ? COPY : 16> B;
+  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128, COPIERS = 256;     // threads that copy a step
+  typedef Operand<T, false, S::TM, COPIERS, KBYTES, COPY ? COPY : 16> A;
+  typedef Operand<T, false, S::TN, COPIERS, KBYTES, COPY ? COPY : 16> B;
   constexpr int LDS = (COPY ? S::RING : 2) * (A::BYTES + B::BYTES);
   a.tiles_m = (a.k + S::TM - 1) / S::TM;
   a.tiles_n = (a.l + S::TN - 1) / S::TN;

@@ -99,9 +99,9 @@ __device__ __forceinline__ void store_tile(const GroupedArgs& a, const RowTile& 
 // Workgroup `block` of the product's grid, split `split` of its inner dimension.
 template <typename T, class S, bool BT, int COPY, bool ADAPT>
 __device__ __forceinline__ void tile_product(const GroupedArgs& a, int block, int split) {
-  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
-  typedef Operand<T, true, S::TM, S::THREADS, KBYTES, COPY ? COPY : 16> A;
-  typedef Operand<T, BT, S::TN, S::THREADS, KBYTES, COPY ? COPY : 16> B;
+  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128, COPIERS = 256;     // threads that copy a step
+  typedef Operand<T, true, S::TM, COPIERS, KBYTES, COPY ? COPY : 16> A;
+  typedef Operand<T, BT, S::TN, COPIERS, KBYTES, COPY ? COPY : 16> B;
   constexpr bool DIRECT = COPY != 0;           // through LDS without registers
   constexpr int KSTEP = A::KSTEP, EPC = A::EPC, THREADS = S::THREADS;
   constexpr int E = DIRECT ? COPY / static_cast<int>(sizeof(T)) : 1;
@@ -201,28 +201,28 @@ __device__ __forceinline__ void tile_product(const GroupedArgs& a, int block, in
 
   auto issue = [&](int step, unsigned int to) {
     const int k0 = k_first + step * KSTEP;
-    to += wave * 64 * COPY;
+    to += (wave & 3) * 64 * COPY;
     if (ADAPT && step >= own_steps) {
       // (few steps with long addresses: not unrolled where there are many copies)
 #pragma unroll COPY == 16 ? 4 : 1
-      for (int i = 0; i < A::PER; ++i) copy_to_lds<COPY>(piece_of_u(step, i), to + i * THREADS * COPY);
+      for (int i = 0; i < A::PER; ++i) copy_to_lds<COPY>(piece_of_u(step, i), to + i * COPIERS * COPY);
 #pragma unroll COPY == 16 ? 4 : 1
       for (int i = 0; i < B::PER; ++i) {
         const T* row = row_of_b(step, i);
-        copy_to_lds<COPY>(row ? static_cast<const void*>(row + min(n0 + B::element_of(i), a.N - E)) : &g_zeros, to + A::BYTES + i * THREADS * COPY);
+        copy_to_lds<COPY>(row ? static_cast<const void*>(row + min(n0 + B::element_of(i), a.N - E)) : &g_zeros, to + A::BYTES + i * COPIERS * COPY);
       }
     } else if (k0 + KSTEP <= k_end) {
 #pragma unroll
-      for (int i = 0; i < A::PER; ++i) copy_to_lds<COPY>(pa[i] + k0, to + i * THREADS * COPY);
+      for (int i = 0; i < A::PER; ++i) copy_to_lds<COPY>(pa[i] + k0, to + i * COPIERS * COPY);
 #pragma unroll
-      for (int i = 0; i < B::PER; ++i) copy_to_lds<COPY>(pb[i] + k0 * step_b, to + A::BYTES + i * THREADS * COPY);
+      for (int i = 0; i < B::PER; ++i) copy_to_lds<COPY>(pb[i] + k0 * step_b, to + A::BYTES + i * COPIERS * COPY);
     } else {
 #pragma unroll
       for (int i = 0; i < A::PER; ++i)
-        copy_to_lds<COPY>(k0 + va[i] < k_end ? static_cast<const void*>(pa[i] + k0) : &g_zeros, to + i * THREADS * COPY);
+        copy_to_lds<COPY>(k0 + va[i] < k_end ? static_cast<const void*>(pa[i] + k0) : &g_zeros, to + i * COPIERS * COPY);
 #pragma unroll
       for (int i = 0; i < B::PER; ++i)
-        copy_to_lds<COPY>(k0 + vb[i] < k_end ? static_cast<const void*>(pb[i] + k0 * step_b) : &g_zeros, to + A::BYTES + i * THREADS * COPY);
+        copy_to_lds<COPY>(k0 + vb[i] < k_end ? static_cast<const void*>(pb[i] + k0 * step_b) : &g_zeros, to + A::BYTES + i * COPIERS * COPY);
     }
   };
   // Up to here all 16 bytes of a piece may be read: a row of X ends behind it; a row of W may end inside it, but another follows.
@@ -277,7 +277,7 @@ __device__ __forceinline__ void tile_product(const GroupedArgs& a, int block, in
       for (int j = 0; j < S::NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (steps > 0) {
       if constexpr (DIRECT && THREADS == 512) {
-        multiply_in_turns<T, S, A, B>(lds, steps, issue, acc, nothing);
+        multiply_in_turns<T, S, A, B>(lds, (steps + 1) >> 1, issue, acc, nothing);     // (a block behind the last one is zeros)
       } else if constexpr (DIRECT) {
         multiply_steps<T, S, A, B, S::RING>(lds, steps, issue, acc, nothing);
       } else {
@@ -344,9 +344,9 @@ void set_tiles(GroupedArgs& a, int tm, int tn, int step, bool one, int splits) {
 }
 
 template <typename T, class S, bool BT, int COPY, bool ADAPT> int launch(GroupedArgs a, int splits, hipStream_t s) {
-  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128;
-  typedef Operand<T, true, S::TM, S::THREADS, KBYTES, COPY ? COPY : 16> A;
-  typedef Operand<T, BT, S::TN, S::THREADS, KBYTES, COPY ? COPY : 16> B;
+  constexpr int KBYTES = S::THREADS == 512 ? 64 : 128, COPIERS = 256;     // threads that copy a step
+  typedef Operand<T, true, S::TM, COPIERS, KBYTES, COPY ? COPY : 16> A;
+  typedef Operand<T, BT, S::TN, COPIERS, KBYTES, COPY ? COPY : 16> B;
   constexpr int LDS = (COPY ? S::RING : 2) * (A::BYTES + B::BYTES);
   set_tiles(a, S::TM, S::TN, A::KSTEP, ADAPT, splits);
   const int64_t blocks = static_cast<int64_t>(a.tiles_n) * a.row_tiles;
