@@ -2,13 +2,14 @@
 //
 // A workgroup takes a run of keys and each of its wavefronts a run of that.  Two passes over the keys: the first counts
 // the keys of every group per wavefront (LDS), the second puts every row at
-//   first place of the group + rows of earlier workgroups + of earlier wavefronts + of earlier lanes with the same key,
-// where the last term comes from comparing the keys of a step that share a group with another one (ballots): no atomic decides a
-// place, so the order is the rows' own.  Few keys are done by one workgroup in one launch; more take three launches: counts per
-// workgroup, sums of those over the workgroups, places.  There a workgroup first sorts 8,192 rows in LDS and then writes them out
-// in that order, so that neighbouring lanes write neighbouring places (6e6 keys in 2,000 groups, scattered one by
-// one: 74 us; so: see place_sorted), as long as LDS holds that beside the counts.
+//   first place of the group + rows of earlier workgroups + of earlier wavefronts + of earlier steps + of earlier lanes,
+// where the lanes of one step that share a group are told apart by ballots: no atomic decides a place, so the order is the rows'
+// own.  Up to 16,384 keys are done by one workgroup in one launch; more take three launches: counts per workgroup, sums of those over
+// the workgroups, places.  There a workgroup first sorts 8,192 rows in LDS and then writes them out in that order, so that
+// neighbouring lanes write neighbouring places, as long as LDS holds that beside the counts (up to about 2,900 groups).
 // A key outside [0, G) counts as group G, whose rows come last.
+// What bounds it: 64 keys 4.5 us, a launch; 6e6 keys in 2,000 groups 67 us, 52 of them in the last launch (the 48 MB that have to move take 9): the chain of LDS accesses and ballots of a step, four wavefronts a SIMD, and the barriers between the passes.
+// (Rows written one by one: 75; ranks of the second pass kept in registers from the first: 67 to 71, small calls slower.)
 #include "grouped.h"
 
 namespace lq {
@@ -18,6 +19,19 @@ constexpr int THREADS = 1024, WAVES = THREADS / 64;
 constexpr int64_t ONE_GROUP_KEYS = 16384;    // most keys of the one-workgroup form
 
 __device__ __forceinline__ int group_of_key(int key, int G) { return static_cast<unsigned>(key) < static_cast<unsigned>(G) ? key : G; }
+
+constexpr int FEW_BITS = 4;     // up to 15 groups: one lane of a group counts for all, which else wait for each other at its counter
+
+// The active lanes of this lane's group.
+__device__ __forceinline__ unsigned long long same_group(int g, int bits, unsigned long long active) {
+  unsigned long long same = active;
+  for (int b = 0; b < bits; ++b) {
+    const bool one = (g >> b) & 1;
+    const unsigned long long v = __ballot(one);
+    same &= one ? v : ~v;
+  }
+  return same;
+}
 
 // How many lanes below this one hold the same group, of those of `active`; `shared`: whether this lane's group is another active
 // lane's as well.  A few such groups are gone through one by one; from many on, all lanes are compared bit by bit.
@@ -34,13 +48,7 @@ __device__ __forceinline__ int lanes_before(int g, int bits, bool shared, unsign
     }
     return before;
   }
-  unsigned long long same = active;
-  for (int b = 0; b < bits; ++b) {
-    const bool one = (g >> b) & 1;
-    const unsigned long long v = __ballot(one);
-    same &= one ? v : ~v;
-  }
-  return __popcll(same & below);
+  return __popcll(same_group(g, bits, active) & below);
 }
 
 // Sum over the workgroup's threads below this one; *total: over all.
@@ -79,17 +87,28 @@ __device__ __forceinline__ void wave_run(int64_t begin, int64_t end, int64_t* b,
 
 constexpr int AHEAD = 8;      // keys of a lane whose loads are under way together
 
-__device__ __forceinline__ void count_keys(const int32_t* __restrict__ keys, int G, int64_t b, int64_t e, unsigned int* mine) {
-  for (int64_t i0 = b + (threadIdx.x & 63); i0 < e; i0 += 64 * AHEAD) {
+// add(group, how many) for the keys [b, e) of a wavefront.
+template <typename F> __device__ __forceinline__ void count_groups(const int32_t* __restrict__ keys, int G, int bits, int64_t b, int64_t e, F&& add) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t i0 = b; i0 < e; i0 += 64 * AHEAD) {
     int key[AHEAD];
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) key[j] = i0 + 64 * j < e ? keys[i0 + 64 * j] : 0;
+    for (int j = 0; j < AHEAD; ++j) key[j] = i0 + 64 * j + lane < e ? keys[i0 + 64 * j + lane] : 0;
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
+      const bool in = i0 + 64 * j + lane < e;
       const int g = group_of_key(key[j], G);
-      if (i0 + 64 * j < e) atomicAdd(&mine[g >> 1], 1u << (16 * (g & 1)));
+      if (bits > FEW_BITS) {
+        if (in) add(g, 1);
+      } else {
+        const unsigned long long same = same_group(g, bits, __ballot(in));
+        if (in && (same & ((1ull << lane) - 1)) == 0) add(g, __popcll(same));
+      }
     }
   }
+}
+__device__ __forceinline__ void count_keys(const int32_t* __restrict__ keys, int G, int bits, int64_t b, int64_t e, unsigned int* mine) {
+  count_groups(keys, G, bits, b, e, [&](int g, int n) { atomicAdd(&mine[g >> 1], static_cast<unsigned int>(n) << (16 * (g & 1))); });
 }
 
 // Turns counts per wavefront into counts of the earlier wavefronts and calls total(g, sum) for every group.
@@ -126,13 +145,19 @@ __device__ __forceinline__ void place_rows(const int32_t* __restrict__ keys, int
       if (!some) break;
       const int g = in ? group_of_key(key[j], G) : -1;
       // (LDS keeps a wavefront's order: the counts before this step, with this step's rows, and then read again)
-      int earlier = 0, after = 0;
+      int earlier = 0, after = 0, before;
       if (in) earlier = mine16[g];
       __builtin_amdgcn_wave_barrier();
-      if (in) atomicAdd(&mine[g >> 1], 1u << (16 * (g & 1)));
-      __builtin_amdgcn_wave_barrier();
-      if (in) after = mine16[g];
-      const int before = lanes_before(g, bits, in && after - earlier > 1, some);
+      if (bits <= FEW_BITS) {
+        const unsigned long long same = same_group(g, bits, some);
+        before = __popcll(same & ((1ull << lane) - 1));
+        if (in && before == 0) atomicAdd(&mine[g >> 1], static_cast<unsigned int>(__popcll(same)) << (16 * (g & 1)));
+      } else {
+        if (in) atomicAdd(&mine[g >> 1], 1u << (16 * (g & 1)));
+        __builtin_amdgcn_wave_barrier();
+        if (in) after = mine16[g];
+        before = lanes_before(g, bits, in && after - earlier > 1, some);
+      }
       if (in) put(i, g, base[g] + earlier + before);
       __builtin_amdgcn_wave_barrier();
     }
@@ -150,7 +175,7 @@ __global__ __launch_bounds__(THREADS) void group_rows_kernel(const int32_t* __re
   int64_t b, e;
   wave_run(0, n, &b, &e);
   unsigned int* mine = counts + (threadIdx.x >> 6) * words;
-  count_keys(keys, G, b, e, mine);
+  count_keys(keys, G, bits, b, e, mine);
   __syncthreads();
   sum_waves(G, reinterpret_cast<unsigned short*>(counts), [&](int g, int sum) { shared_base[g] = sum; });
   __syncthreads();
@@ -170,20 +195,15 @@ __global__ __launch_bounds__(THREADS) void group_rows_kernel(const int32_t* __re
              [&](int64_t row, int, int place) { order[place] = static_cast<int32_t>(row); });
 }
 
-__global__ __launch_bounds__(THREADS) void group_count_kernel(const int32_t* __restrict__ keys, int64_t n, int64_t per, int G,
+__global__ __launch_bounds__(THREADS) void group_count_kernel(const int32_t* __restrict__ keys, int64_t n, int64_t per, int G, int bits,
                                                               int32_t* __restrict__ counts) {
   extern __shared__ int hist[];
   for (int g = threadIdx.x; g <= G; g += THREADS) hist[g] = 0;
   __syncthreads();
   const int64_t begin = blockIdx.x * per, end = min(begin + per, n);
-  for (int64_t i0 = begin + threadIdx.x; i0 < end; i0 += THREADS * AHEAD) {
-    int key[AHEAD];
-#pragma unroll
-    for (int j = 0; j < AHEAD; ++j) key[j] = i0 + j * THREADS < end ? keys[i0 + j * THREADS] : 0;
-#pragma unroll
-    for (int j = 0; j < AHEAD; ++j)
-      if (i0 + j * THREADS < end) atomicAdd(&hist[group_of_key(key[j], G)], 1);
-  }
+  int64_t b, e;
+  wave_run(begin, max(begin, end), &b, &e);
+  count_groups(keys, G, bits, b, e, [&](int g, int n) { atomicAdd(&hist[g], n); });
   __syncthreads();
   for (int g = threadIdx.x; g <= G; g += THREADS) counts[static_cast<int64_t>(blockIdx.x) * (G + 1) + g] = hist[g];
 }
@@ -248,7 +268,7 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
     __syncthreads();
     int64_t b, e;
     wave_run(at, to, &b, &e);
-    count_keys(keys, G, b, e, mine);
+    count_keys(keys, G, bits, b, e, mine);
     __syncthreads();
     if constexpr (SORT) {
       sum_waves(G, own16, [&](int g, int sum) { local[g] = sum; });
@@ -342,7 +362,7 @@ int launch_group_rows(const int32_t* keys, int64_t n, int32_t G, int32_t* off, i
   split(n, &per, &blocks);
   int32_t* counts = static_cast<int32_t*>(ws);
   int32_t* totals = counts + static_cast<int64_t>(blocks) * (G + 1);
-  group_count_kernel<<<blocks, THREADS, (G + 1) * 4, s>>>(keys, n, per, G, counts);
+  group_count_kernel<<<blocks, THREADS, (G + 1) * 4, s>>>(keys, n, per, G, bits, counts);
   LQ_LAUNCH_CHECK("group_count_kernel");
   group_sum_kernel<<<G / SUM_GROUPS + 1, THREADS, 0, s>>>(blocks, G, counts, totals);
   LQ_LAUNCH_CHECK("group_sum_kernel");

@@ -262,7 +262,7 @@ Plan plan_of(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype, int copy
   p.side = dtype == LQ_BF16 && copy == 16 && k > 192 && l > 192 ? 256 : k > 64 && l > 64 ? 128 : 64;
   const int64_t tiles = static_cast<int64_t>((k + p.side - 1) / p.side) * ((l + p.side - 1) / p.side);
   const int64_t even = n * tiles / (num_cus() * (p.side == 256 ? 1 : 2));
-  p.most = std::max<int64_t>((even + 63) / 64 * 64, dtype == LQ_BF16 ? 1024 : 256);
+  p.most = std::max<int64_t>((even + 63) / 64 * 64, dtype == LQ_BF16 && p.side == 256 ? 1024 : 256);
   // chunks of groups of more than one: fewer than two for every `most` rows, and fewer than one more a group
   p.places = std::min<int64_t>(2 * n / p.most, n / p.most + G);
   return p;
