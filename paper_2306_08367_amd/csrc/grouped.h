@@ -52,7 +52,8 @@ size_t group_rows_ws_bytes(int64_t n, int32_t G);
 int launch_check_groups(const lq_groups& g, int32_t* flag, hipStream_t s);
 int launch_check_keys(const int32_t* keys, int64_t n, int32_t G, int32_t* flag, hipStream_t s);
 // `copy`: rows of X and of the matrices may be read in pieces of 16 or 4 bytes, aligned to that, or only element by element (0).
-int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed, int copy, hipStream_t s);
+size_t grouped_product_ws_bytes(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype);
+int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed, int copy, void* ws, size_t ws_bytes, hipStream_t s);
 // `main`: everything but U, rp, u_rest and group_of, which the call puts into the workspace (256 bytes in).
 size_t adapter_ws_bytes(int64_t n, int32_t G, int32_t k, int32_t l, int32_t rank, int32_t dtype);
 int launch_adapter_product(const GroupedArgs& main, const lq_stack& A, const float* scale, void* ws, int32_t dtype, int main_copy, int low_copy,

@@ -113,8 +113,8 @@ int lq_group_rows(const int32_t* keys, int64_t n, int32_t n_groups, int32_t* off
 }
 
 size_t lq_grouped_workspace_bytes(int64_t n, int32_t n_groups, int32_t k, int32_t l, int32_t dtype) {
-  (void)n; (void)n_groups; (void)k; (void)l; (void)dtype;
-  return 0;
+  if (n < 0 || n > MAX_POSITIONS || n_groups < 1 || n_groups > LQ_MAX_MODELS || k < 1 || l < 1 || !dtype_ok(dtype)) return 0;
+  return grouped_product_ws_bytes(n, n_groups, k, l, dtype);
 }
 size_t lq_grouped_gradient_workspace_bytes(int64_t n, int32_t n_groups, int32_t k, int32_t l, int32_t dtype) {
   if (n < 0 || n > MAX_POSITIONS || n_groups < 1 || n_groups > LQ_MAX_MODELS || k < 1 || l < 1 || !dtype_ok(dtype)) return 0;
@@ -166,7 +166,8 @@ int lq_grouped_product(const lq_groups* groups, const lq_mat* X, int32_t x_slots
   a.relu = (flags & LQ_RELU) != 0;
   a.y_vec = aligned_rows(Y->data, Y->ld, Y->dtype) && (!gate || aligned_rows(gate->data, gate->ld, gate->dtype)) &&
             (!bias || aligned_rows(bias->data, bias->ld, bias->dtype));
-  return launch_grouped_product(a, X->dtype, transposed, std::min(piece_bytes(*X), piece_bytes(*W)), s);
+  if (ws && !aligned(ws, 256)) return fail(LQ_ERR_WORKSPACE, "lq_grouped_product: the workspace is not 256-byte aligned");
+  return launch_grouped_product(a, X->dtype, transposed, std::min(piece_bytes(*X), piece_bytes(*W)), ws, ws_bytes, s);
 }
 
 int lq_grouped_gradient(const lq_groups* groups, const lq_mat* X, int32_t x_slots, const lq_mat* dY, lq_stack* dW, lq_mat* db,

@@ -472,6 +472,47 @@ __global__ __launch_bounds__(256) void adapter_finish_kernel(GroupedArgs a, cons
   else store_four<false>(a.Y, static_cast<int64_t>(r) * a.ldy + n, valid, y);
 }
 
+// Adds up the partial sums of a product in splits: one position and 1,024 columns a workgroup.
+template <typename T> __global__ __launch_bounds__(256) void grouped_finish_kernel(GroupedArgs a, const float* __restrict__ sums, int splits) {
+  constexpr int AHEAD = 8;
+  const int p = blockIdx.x, n = blockIdx.y * 1024 + 4 * threadIdx.x, valid = a.N - n;
+  if (valid <= 0) return;
+  const float* sum = sums + static_cast<int64_t>(p) * a.N + n;
+  const int64_t stride = static_cast<int64_t>(a.n) * a.N;
+  f32x4 part[AHEAD], y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int z = 0; z < AHEAD; ++z) part[z] = load_four(sum + min(z, splits - 1) * stride, valid);
+  const int g = a.group_of[p];
+  const int64_t r = a.y_grouped || !a.order ? p : a.order[p];
+#pragma unroll
+  for (int z = 0; z < AHEAD; ++z)
+    if (z < splits) y += part[z];
+  for (int z = AHEAD; z < splits; ++z) y += load_four(sum + z * stride, valid);
+  if (a.bias && g >= 0) y += load_four(static_cast<const T*>(a.bias) + g * a.ldb + n, valid);
+  if (a.relu)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] = y[q] < 0.f ? 0.f : y[q];
+  if (a.gate) {
+    const f32x4 h = load_four(static_cast<const T*>(a.gate) + r * a.ldg + n, valid);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] = h[q] > 0.f ? y[q] : 0.f;
+  }
+  if (a.y_bf16) store_four<true>(a.Y, r * a.ldy + n, valid, y);
+  else store_four<false>(a.Y, r * a.ldy + n, valid, y);
+}
+
+// Splits of the inner dimension of a grouped product: where its tiles of 64 x 64 fill less than half of the compute units and have many
+// steps, so that the second launch is worth it (320 rows in 10 groups, 3,509 -> 53 in bf16: 45 us in one split).  At least four steps each.
+int product_splits(int64_t n, int32_t G, int32_t K, int32_t N, int32_t dtype) {
+  const int64_t tiles = (n / 64 + std::min<int64_t>(n, G + 1)) * ((N + 63) / 64), steps = (K * static_cast<int64_t>(dtype_size(dtype)) + 127) / 128;
+  if (n == 0 || tiles > 128 || steps < 32) return 1;
+  return static_cast<int>(std::min<int64_t>({512 / tiles, steps / 4, 16}));
+}
+// (the group of every position, then the partial sums)
+size_t split_bytes(int64_t n, int32_t N, int splits) {
+  return splits < 2 ? 0 : round_up(static_cast<size_t>(n) * 4, 256) + round_up(static_cast<size_t>(splits) * n * N * 4, 256);
+}
+
 // How an adapter product runs, and what lies where in its workspace behind the first 256 bytes (kept for LQ_CHECK_FKS).
 //   few rows    the products of X with W and with A in one launch of tiles of 64 x 64, both in splits of the inner dimension so that
 //               there are two tiles a compute unit, then adapter_finish_kernel: where W alone has at most one tile a compute unit and
@@ -540,8 +581,33 @@ template <typename T> int few_rows(const GroupedArgs& m, GroupedArgs low, const 
 
 }  // namespace
 
-int launch_grouped_product(const GroupedArgs& a, int32_t dtype, bool transposed, int copy, hipStream_t s) {
-  return dtype == LQ_BF16 ? product<bf16_t>(a, transposed, copy, 1, s) : product<float>(a, transposed, copy, 1, s);
+size_t grouped_product_ws_bytes(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype) {
+  return std::max(split_bytes(n, l, product_splits(n, G, k, l, dtype)), split_bytes(n, k, product_splits(n, G, l, k, dtype)));
+}
+
+int launch_grouped_product(const GroupedArgs& args, int32_t dtype, bool transposed, int copy, void* ws, size_t ws_bytes, hipStream_t s) {
+  GroupedArgs a = args;
+  const int splits = product_splits(a.n, a.G, a.K, a.N, dtype);
+  if (splits < 2 || !ws || ws_bytes < split_bytes(a.n, a.N, splits))
+    return dtype == LQ_BF16 ? product<bf16_t>(a, transposed, copy, 1, s) : product<float>(a, transposed, copy, 1, s);
+  a.gpos = static_cast<int32_t*>(ws);
+  a.Y = static_cast<char*>(ws) + round_up(static_cast<size_t>(a.n) * 4, 256);
+  a.ldy = a.N;
+  a.split_stride = static_cast<int64_t>(a.n) * a.N;
+  a.y_grouped = 1;
+  a.y_bf16 = 0;
+  a.y_vec = a.N % 4 == 0;
+  a.bias = a.gate = nullptr;
+  a.relu = 0;
+  const int rc = dtype == LQ_BF16 ? product<bf16_t>(a, transposed, copy, splits, s) : product<float>(a, transposed, copy, splits, s);
+  if (rc) return rc;
+  GroupedArgs f = args;
+  f.group_of = a.gpos;
+  const dim3 grid(f.n, (f.N + 1023) / 1024);
+  if (dtype == LQ_BF16) grouped_finish_kernel<bf16_t><<<grid, 256, 0, s>>>(f, static_cast<const float*>(a.Y), splits);
+  else grouped_finish_kernel<float><<<grid, 256, 0, s>>>(f, static_cast<const float*>(a.Y), splits);
+  LQ_LAUNCH_CHECK("grouped_finish_kernel");
+  return LQ_OK;
 }
 
 size_t adapter_ws_bytes(int64_t n, int32_t G, int32_t k, int32_t l, int32_t rank, int32_t dtype) { return adapter_plan(n, G, k, l, rank, dtype).bytes; }

@@ -161,6 +161,16 @@ def test_product_row_orders(lq, dtype, how, more):
     _run_product(lq, 40, 9, 96, 81, dtype, how=how, integers=True, **more)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,G,k,l", [(1, 1, 4100, 8), (5, 3, 2053, 70), (320, 10, 3509, 53), (60, 64, 4096, 64), (33, 2, 2500, 300)])
+def test_products_of_few_rows_over_a_long_inner_dimension(lq, n, G, k, l, dtype):
+    """These run in splits of the inner dimension, whose partial sums a second launch adds up."""
+    for how in ("ragged", "even", "none"):
+        _run_product(lq, n, G, k, l, dtype, how=how, integers=True, bias=True, relu=True, gate=True)
+        _run_product(lq, n, G, l, k, dtype, how=how, integers=True, transposed=True, gate=True, y_grouped=True, out=F32)
+        _run_product(lq, n, G, k, l, dtype, how=how, slots=2, bias=True)
+
+
 def test_products_of_many_rows(lq):
     for dtype, n in ((BF16, 40_000), (F32, 20_000)):
         for transposed in (False, True):
