@@ -601,10 +601,11 @@ typedef struct {
 /* Which rows belong to which group.  Position p, for offsets[g] <= p < offsets[g + 1], holds row
  * order[p] of group g; positions from offsets[n_groups] to n hold the rows without a group. */
 typedef struct {
-  int64_t        n;        /* positions, < 2^31 */
+  int64_t        n;        /* positions, at most 2^30; so are the widths of all matrices */
   int32_t        n_groups; /* 1..LQ_MAX_MODELS */
   const int32_t* offsets;  /* device, [n_groups + 1], ascending, offsets[0] = 0, last one <= n */
-  const int32_t* order;    /* device, [n], each value of 0 .. n - 1 once; NULL: order[p] = p */
+  const int32_t* order;    /* device, [n], each value of 0 .. n - 1 once (of a row named twice, one of the
+                            * results stays); NULL: order[p] = p */
 } lq_groups;
 
 /* flags of the grouped calls */
@@ -671,7 +672,7 @@ size_t lq_grouped_gradient_workspace_bytes(int64_t n, int32_t n_groups, int32_t 
  *   X [n x k], W [k x l], A n_groups matrices [k x rank], B n_groups matrices [rank x l], all of one type;
  *   rank 1..LQ_MAX_RANK;  bias NULL or [1 x l] of that type;  scale device fp32 [n_groups] or NULL (all 1)
  *   Y [n x l], of that type (or f32 when that is bf16); must not overlap an input
- *   The products X A_g are kept in fp32.
+ *   The products X A_g are kept in fp32.  An adapter's infinities and NaNs reach the rows of its own group only.
  *   flags  0 or LQ_CHECK_FKS;  ws  lq_adapter_workspace_bytes(..) bytes, 256-byte aligned, required
  */
 int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W, const lq_mat* bias,

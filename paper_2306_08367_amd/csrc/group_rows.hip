@@ -20,7 +20,9 @@ constexpr int64_t ONE_GROUP_KEYS = 16384;    // most keys of the one-workgroup f
 
 __device__ __forceinline__ int group_of_key(int key, int G) { return static_cast<unsigned>(key) < static_cast<unsigned>(G) ? key : G; }
 
-constexpr int FEW_BITS = 4;     // up to 15 groups: one lane of a group counts for all, which else wait for each other at its counter
+// Up to 15 groups over many keys: one lane of a group counts for all, which else wait for each other at its counter (2.3e6 keys in 7
+// groups 54 -> 38 us; instantiations of their own, since the code of both ways took a call of 64 keys from 4.7 to 6.7 us).
+constexpr int FEW_BITS = 4;
 
 // The active lanes of this lane's group.
 __device__ __forceinline__ unsigned long long same_group(int g, int bits, unsigned long long active) {
@@ -88,7 +90,7 @@ __device__ __forceinline__ void wave_run(int64_t begin, int64_t end, int64_t* b,
 constexpr int AHEAD = 8;      // keys of a lane whose loads are under way together
 
 // add(group, how many) for the keys [b, e) of a wavefront.
-template <typename F> __device__ __forceinline__ void count_groups(const int32_t* __restrict__ keys, int G, int bits, int64_t b, int64_t e, F&& add) {
+template <bool FEW, typename F> __device__ __forceinline__ void count_groups(const int32_t* __restrict__ keys, int G, int bits, int64_t b, int64_t e, F&& add) {
   const int lane = threadIdx.x & 63;
   for (int64_t i0 = b; i0 < e; i0 += 64 * AHEAD) {
     int key[AHEAD];
@@ -98,7 +100,7 @@ template <typename F> __device__ __forceinline__ void count_groups(const int32_t
     for (int j = 0; j < AHEAD; ++j) {
       const bool in = i0 + 64 * j + lane < e;
       const int g = group_of_key(key[j], G);
-      if (bits > FEW_BITS) {
+      if constexpr (!FEW) {
         if (in) add(g, 1);
       } else {
         const unsigned long long same = same_group(g, bits, __ballot(in));
@@ -107,8 +109,8 @@ template <typename F> __device__ __forceinline__ void count_groups(const int32_t
     }
   }
 }
-__device__ __forceinline__ void count_keys(const int32_t* __restrict__ keys, int G, int bits, int64_t b, int64_t e, unsigned int* mine) {
-  count_groups(keys, G, bits, b, e, [&](int g, int n) { atomicAdd(&mine[g >> 1], static_cast<unsigned int>(n) << (16 * (g & 1))); });
+template <bool FEW> __device__ __forceinline__ void count_keys(const int32_t* __restrict__ keys, int G, int bits, int64_t b, int64_t e, unsigned int* mine) {
+  count_groups<FEW>(keys, G, bits, b, e, [&](int g, int n) { atomicAdd(&mine[g >> 1], static_cast<unsigned int>(n) << (16 * (g & 1))); });
 }
 
 // Turns counts per wavefront into counts of the earlier wavefronts and calls total(g, sum) for every group.
@@ -128,7 +130,7 @@ template <typename F> __device__ __forceinline__ void sum_waves(int G, unsigned 
 }
 
 // put(row, group, place) for the rows of the wavefront's run, in their order; base: first places of the groups.
-template <typename F>
+template <bool FEW, typename F>
 __device__ __forceinline__ void place_rows(const int32_t* __restrict__ keys, int G, int bits, int64_t b, int64_t e, const int* base,
                                            unsigned int* mine, F&& put) {
   const int lane = threadIdx.x & 63;
@@ -148,7 +150,7 @@ __device__ __forceinline__ void place_rows(const int32_t* __restrict__ keys, int
       int earlier = 0, after = 0, before;
       if (in) earlier = mine16[g];
       __builtin_amdgcn_wave_barrier();
-      if (bits <= FEW_BITS) {
+      if constexpr (FEW) {
         const unsigned long long same = same_group(g, bits, some);
         before = __popcll(same & ((1ull << lane) - 1));
         if (in && before == 0) atomicAdd(&mine[g >> 1], static_cast<unsigned int>(__popcll(same)) << (16 * (g & 1)));
@@ -175,7 +177,7 @@ __global__ __launch_bounds__(THREADS) void group_rows_kernel(const int32_t* __re
   int64_t b, e;
   wave_run(0, n, &b, &e);
   unsigned int* mine = counts + (threadIdx.x >> 6) * words;
-  count_keys(keys, G, bits, b, e, mine);
+  count_keys<false>(keys, G, bits, b, e, mine);
   __syncthreads();
   sum_waves(G, reinterpret_cast<unsigned short*>(counts), [&](int g, int sum) { shared_base[g] = sum; });
   __syncthreads();
@@ -191,11 +193,11 @@ __global__ __launch_bounds__(THREADS) void group_rows_kernel(const int32_t* __re
     first += total;
   }
   __syncthreads();
-  place_rows(keys, G, bits, b, e, shared_base, mine,
+  place_rows<false>(keys, G, bits, b, e, shared_base, mine,
              [&](int64_t row, int, int place) { order[place] = static_cast<int32_t>(row); });
 }
 
-__global__ __launch_bounds__(THREADS) void group_count_kernel(const int32_t* __restrict__ keys, int64_t n, int64_t per, int G, int bits,
+template <bool FEW> __global__ __launch_bounds__(THREADS) void group_count_kernel(const int32_t* __restrict__ keys, int64_t n, int64_t per, int G, int bits,
                                                               int32_t* __restrict__ counts) {
   extern __shared__ int hist[];
   for (int g = threadIdx.x; g <= G; g += THREADS) hist[g] = 0;
@@ -203,7 +205,7 @@ __global__ __launch_bounds__(THREADS) void group_count_kernel(const int32_t* __r
   const int64_t begin = blockIdx.x * per, end = min(begin + per, n);
   int64_t b, e;
   wave_run(begin, max(begin, end), &b, &e);
-  count_groups(keys, G, bits, b, e, [&](int g, int n) { atomicAdd(&hist[g], n); });
+  count_groups<FEW>(keys, G, bits, b, e, [&](int g, int n) { atomicAdd(&hist[g], n); });
   __syncthreads();
   for (int g = threadIdx.x; g <= G; g += THREADS) counts[static_cast<int64_t>(blockIdx.x) * (G + 1) + g] = hist[g];
 }
@@ -237,7 +239,7 @@ __global__ __launch_bounds__(THREADS) void group_sum_kernel(int blocks, int G, i
 constexpr int SORTED = THREADS * AHEAD;
 inline size_t sorted_lds(int G) { return place_lds(G) + (static_cast<size_t>(G) + 1) * 4 + SORTED * 4; }
 
-template <bool SORT>
+template <bool SORT, bool FEW>
 __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __restrict__ keys, int64_t n, int64_t per, int G, int bits,
                                                               const int32_t* __restrict__ counts, const int32_t* __restrict__ totals,
                                                               int32_t* __restrict__ off, int32_t* __restrict__ order) {
@@ -268,7 +270,7 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
     __syncthreads();
     int64_t b, e;
     wave_run(at, to, &b, &e);
-    count_keys(keys, G, bits, b, e, mine);
+    count_keys<FEW>(keys, G, bits, b, e, mine);
     __syncthreads();
     if constexpr (SORT) {
       sum_waves(G, own16, [&](int g, int sum) { local[g] = sum; });
@@ -282,7 +284,7 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
         before_all += total;
       }
       __syncthreads();
-      place_rows(keys, G, bits, b, e, local, mine, [&](int64_t r, int g, int place) {
+      place_rows<FEW>(keys, G, bits, b, e, local, mine, [&](int64_t r, int g, int place) {
         row[place] = static_cast<unsigned short>(r - at);
         group[place] = static_cast<unsigned short>(g);
       });
@@ -297,7 +299,7 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
     } else {
       sum_waves(G, own16, [](int, int) {});
       __syncthreads();
-      place_rows(keys, G, bits, b, e, next, mine,
+      place_rows<FEW>(keys, G, bits, b, e, next, mine,
                  [&](int64_t r, int, int place) { order[place] = static_cast<int32_t>(r); });
     }
   }
@@ -362,13 +364,14 @@ int launch_group_rows(const int32_t* keys, int64_t n, int32_t G, int32_t* off, i
   split(n, &per, &blocks);
   int32_t* counts = static_cast<int32_t*>(ws);
   int32_t* totals = counts + static_cast<int64_t>(blocks) * (G + 1);
-  group_count_kernel<<<blocks, THREADS, (G + 1) * 4, s>>>(keys, n, per, G, bits, counts);
+  const bool few = bits <= FEW_BITS;
+  (few ? group_count_kernel<true> : group_count_kernel<false>)<<<blocks, THREADS, (G + 1) * 4, s>>>(keys, n, per, G, bits, counts);
   LQ_LAUNCH_CHECK("group_count_kernel");
   group_sum_kernel<<<G / SUM_GROUPS + 1, THREADS, 0, s>>>(blocks, G, counts, totals);
   LQ_LAUNCH_CHECK("group_sum_kernel");
   const bool sort = sorted_lds(G) <= 156 * 1024;
   const size_t bytes = sort ? sorted_lds(G) : lds;
-  const auto kernel = sort ? group_place_kernel<true> : group_place_kernel<false>;
+  const auto kernel = few ? group_place_kernel<true, true> : sort ? group_place_kernel<true, false> : group_place_kernel<false, false>;
   if (bytes > 64 * 1024)
     LQ_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
   kernel<<<blocks, THREADS, bytes, s>>>(keys, n, per, G, bits, counts, totals, off, order);

@@ -7,6 +7,8 @@
 
 namespace lq {
 
+constexpr int64_t MOST_THREADS = 0xffffffffll;     // of a launch
+
 // Everything a product needs, by value as the kernel argument.  The operator is Y[row(p)] = X[row(p)] * W_group(p).
 struct GroupedArgs {
   const int32_t* off;     // [G + 1]; NULL: all positions use the first matrix
@@ -18,7 +20,7 @@ struct GroupedArgs {
   const void* gate; int64_t ldg;
   void* Y; int64_t ldy;
   int32_t K, N;           // inner width and width of the result
-  int32_t n_store;        // columns stored (>= N; those past N are zeros)
+  int32_t n_store;        // columns stored (>= N; those past N hold no result)
   int32_t slots;          // row r of Y reads row r / slots of X
   int32_t x_grouped, y_grouped;
   int32_t relu, y_bf16;
@@ -145,13 +147,9 @@ __device__ __forceinline__ int die_order(int id, int total) {
   return die * per + min(die, more) + at;
 }
 
-// The tile that workgroup `id` works on: TM rows of one group and one of `cols` column tiles.  Tiles are numbered group by
-// group, then those of the rows without a group (group -1); inside a group by runs of 8 row tiles, the rows of a run
-// fastest, so that neighbouring tiles share the rows of X and the columns of the matrix about evenly.  rows == 0: there is
-// no such tile.  Called by a whole wavefront: lane l adds up the row tiles of groups l * per .. l * per + per - 1, the sums are
-// scanned over the lanes, and the lane that holds the tile walks its groups again.
 struct RowTile { int group, first, rows, col; };
-// Tile `local` of positions [begin, end).
+// Tile `local` of positions [begin, end): runs of 8 row tiles, the rows of a run fastest, so that neighbouring tiles share the rows of
+// X and the columns of the matrix about evenly.  rows == 0: there is no such tile.
 template <int TM> __device__ __forceinline__ RowTile tile_of_range(int group, int begin, int end, int local, int cols) {
   constexpr int RUN = 8;
   const int run = local / (RUN * cols), tiles = (end - begin + TM - 1) / TM;
@@ -160,6 +158,10 @@ template <int TM> __device__ __forceinline__ RowTile tile_of_range(int group, in
   const int first = begin + (run * RUN + left % in_run) * TM;
   return {group, first, min(TM, end - first), left / in_run};
 }
+// The tile that workgroup `id` works on: TM rows of one group and one of `cols` column tiles.  Tiles are numbered group by
+// group, then those of the rows without a group (group -1), and shared out evenly over the dies.  Called by a whole wavefront:
+// lane l adds up the row tiles of groups l * per .. l * per + per - 1, the sums are scanned over the lanes, and the lane that holds
+// the tile walks its groups again.
 template <int TM> __device__ __forceinline__ RowTile find_tile(const int32_t* __restrict__ off, int G, int n, int id, int cols) {
   const int lane = threadIdx.x & 63;
   const int per = (G + 63) >> 6;

@@ -5,6 +5,7 @@ namespace lq {
 namespace {
 
 constexpr int64_t MAX_POSITIONS = 1ll << 30;
+constexpr int32_t MAX_WIDTH = 1 << 30;
 
 int check_stack(const lq_stack* w, const char* what, int32_t count, int32_t rows, int32_t cols, bool output) {
   if (!w) return fail(LQ_ERR_NULL, "%s is NULL", what);
@@ -133,6 +134,7 @@ int lq_grouped_product(const lq_groups* groups, const lq_mat* X, int32_t x_slots
   if ((rc = check_stack(W, "W", groups->n_groups, W->rows, W->cols, false))) return rc;
   const int32_t K = transposed ? W->cols : W->rows, N = transposed ? W->rows : W->cols;
   if (K < 1 || N < 1) return fail(LQ_ERR_SHAPE, "W has no rows or no columns");
+  if (K > MAX_WIDTH || N > MAX_WIDTH) return fail(LQ_ERR_SHAPE, "W has more than 2^30 rows or columns");
   const int64_t n = groups->n;
   if (x_slots < 1 || (x_slots > 1 && (transposed || (flags & LQ_X_GROUPED))))
     return fail(LQ_ERR_SHAPE, "x_slots %d: must be 1, or more without LQ_TRANSPOSED and LQ_X_GROUPED", x_slots);
@@ -182,6 +184,7 @@ int lq_grouped_gradient(const lq_groups* groups, const lq_mat* X, int32_t x_slot
     return fail(LQ_ERR_SHAPE, "x_slots %d: must be 1, or more without LQ_X_GROUPED", x_slots);
   if (n % x_slots) return fail(LQ_ERR_SHAPE, "%lld positions are not a multiple of x_slots %d", (long long)n, x_slots);
   if (X->cols < 1 || dY->cols < 1) return fail(LQ_ERR_SHAPE, "X or dY has no columns");
+  if (X->cols > MAX_WIDTH || dY->cols > MAX_WIDTH) return fail(LQ_ERR_SHAPE, "X or dY has more than 2^30 columns");
   if ((rc = check_shape(X, "X", n / x_slots, X->cols))) return rc;
   if ((rc = check_shape(dY, "dY", n, dY->cols))) return rc;
   if (X->dtype != dY->dtype) return fail(LQ_ERR_DTYPE, "X and dY differ in dtype");
@@ -220,7 +223,8 @@ int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W
   if (flags & ~LQ_CHECK_FKS) return fail(LQ_ERR_UNSUPPORTED, "unknown flags 0x%x", flags);
   if (!X || !W || !A || !B || !Y) return fail(LQ_ERR_NULL, "X, W, A, B or Y is NULL");
   const int64_t n = groups->n;
-  if (W->rows < 1 || W->rows > 0x7fffffff || W->cols < 1) return fail(LQ_ERR_SHAPE, "W has no rows or no columns");
+  if (W->rows < 1 || W->cols < 1) return fail(LQ_ERR_SHAPE, "W has no rows or no columns");
+  if (W->rows > MAX_WIDTH || W->cols > MAX_WIDTH) return fail(LQ_ERR_SHAPE, "W has more than 2^30 rows or columns");
   const int32_t k = static_cast<int32_t>(W->rows), l = W->cols, rank = A->cols;
   if (rank < 1 || rank > LQ_MAX_RANK) return fail(LQ_ERR_SHAPE, "rank %d outside 1..%d", rank, LQ_MAX_RANK);
   if ((rc = check_shape(W, "W", k, l))) return rc;

@@ -279,7 +279,7 @@ template <typename T, class S, int COPY> int launch(GradientArgs a, const Plan& 
   const int64_t chunks = a.n / p.most + a.G, tiles = static_cast<int64_t>(a.tiles_m) * a.tiles_n;
   const int64_t run_tiles = std::min<int64_t>(tiles, RUN), runs = chunks * ((tiles + run_tiles - 1) / run_tiles);
   const int64_t blocks = (runs + 7) / 8 * 8 * run_tiles;
-  if (blocks > 0x7fffffff) return fail(LQ_ERR_UNSUPPORTED, "grouped gradient: %lld tiles are more than one launch takes", (long long)blocks);
+  if (blocks * S::THREADS > MOST_THREADS) return fail(LQ_ERR_UNSUPPORTED, "grouped gradient: %lld tiles are more than one launch takes", (long long)blocks);
   const auto kernel = grouped_gradient_kernel<T, S, COPY>;
   if (LDS + SEGMENT * 4 > 48 * 1024)
     LQ_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));

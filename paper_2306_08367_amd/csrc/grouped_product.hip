@@ -350,7 +350,7 @@ template <typename T, class S, bool BT, int COPY, bool ADAPT> int launch(Grouped
   constexpr int LDS = (COPY ? S::RING : 2) * (A::BYTES + B::BYTES);
   set_tiles(a, S::TM, S::TN, A::KSTEP, ADAPT, splits);
   const int64_t blocks = static_cast<int64_t>(a.tiles_n) * a.row_tiles;
-  if (blocks > 0x7fffffff) return fail(LQ_ERR_UNSUPPORTED, "grouped product: %lld tiles are more than one launch takes", (long long)blocks);
+  if (blocks * S::THREADS > MOST_THREADS) return fail(LQ_ERR_UNSUPPORTED, "grouped product: %lld tiles are more than one launch takes", (long long)blocks);
   const auto kernel = grouped_product_kernel<T, S, BT, COPY, ADAPT>;
   if (LDS >= 64 * 1024)
     LQ_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));

@@ -171,6 +171,16 @@ def test_products_of_few_rows_over_a_long_inner_dimension(lq, n, G, k, l, dtype)
         _run_product(lq, n, G, k, l, dtype, how=how, slots=2, bias=True)
 
 
+@pytest.mark.parametrize("n", [3, 900, 6000])
+def test_the_most_groups(lq, n):
+    for dtype in (F32, BF16):
+        _run_product(lq, n, 4096, 16, 24, dtype, integers=True, bias=True)
+        _run_product(lq, n, 4096, 24, 16, dtype, how="one", integers=True, transposed=True)
+        _run_gradient(lq, n, 4096, 16, 24, dtype, integers=True)
+        _run_adapter(lq, n, 4096, 32, 24, 3, dtype, integers=True)
+        _run_adapter(lq, n, 4096, 32, 24, 3, dtype, how="one", integers=True)
+
+
 def test_products_of_many_rows(lq):
     for dtype, n in ((BF16, 40_000), (F32, 20_000)):
         for transposed in (False, True):

@@ -60,7 +60,8 @@ PRODUCT_REFUSALS = [
     ("W.stride", -1, SHAPE, "stride"), ("W.rows", 0, SHAPE, "no rows"), ("W.dtype", 9, DTYPE, "W: unknown"), ("bias.rows", 2, SHAPE, "bias is 2 x 5"),
     ("bias.dtype", 1, DTYPE, "bias"), ("gate.cols", 4, SHAPE, "gate is"), ("gate.dtype", 1, DTYPE, "gate"), ("Y.rows", 13, SHAPE, "Y is 13"),
     ("Y.dtype", 1, DTYPE, "bf16 output"), ("Y.data", None, NULL, "Y: data"), ("Y.ld", 3, SHAPE, "Y: ld"), ("flags", 0x100, UNSUPPORTED, "flags"),
-    ("flags", 1, WORKSPACE, "256"), ("flags", 0x20, SHAPE, "X is 12 x 8, expected 12 x 5"),
+    ("flags", 1, WORKSPACE, "256"), ("flags", 0x20, SHAPE, "X is 12 x 8, expected 12 x 5"), ("W.rows", (1 << 30) + 1, SHAPE, "2^30"),
+    ("ws", FAKE + 8, WORKSPACE, "aligned"),
 ]
 
 
@@ -95,7 +96,7 @@ def test_slots_need_rows_by_number(b):
     ("groups", None, NULL, "groups"), ("X", None, NULL, "X"), ("Y", None, NULL, "dY"), ("W", None, NULL, "dW"), ("X.rows", 3, SHAPE, "X is 3"),
     ("Y.rows", 3, SHAPE, "dY is 3"), ("Y.dtype", 1, DTYPE, "X and dY"), ("W.rows", 7, SHAPE, "dW is"), ("W.stride", 39, SHAPE, "overlap"),
     ("W.dtype", 1, DTYPE, "bf16 output"), ("bias.cols", 4, SHAPE, "db is"), ("bias.dtype", 1, DTYPE, "db and dW"), ("flags", 0x10, UNSUPPORTED, "flags"),
-    ("flags", 1, WORKSPACE, "256"), ("X.cols", 0, SHAPE, "no columns"),
+    ("flags", 1, WORKSPACE, "256"), ("X.cols", 0, SHAPE, "no columns"), ("ws", FAKE + 8, WORKSPACE, "aligned"),
 ])
 def test_gradient_refuses(b, name, value, code, text):
     p = _parts(b)
@@ -128,6 +129,10 @@ def test_workspace_sizes(b):
     small, large = b.lq_group_rows_workspace_bytes(100_000, 8), b.lq_group_rows_workspace_bytes(1 << 30, 4096)
     assert 0 < small < large and small % 256 == 0
     assert b.lq_adapter_workspace_bytes(0, 4, 8, 8, 300, 0) == 0 and b.lq_adapter_workspace_bytes(8, 4, 8, 8, 4, 5) == 0
+    # a few rows over a long inner dimension: partial sums; many rows or a short one: nothing
+    assert b.lq_grouped_workspace_bytes(16, 4, 4096, 64, 1) >= 2 * 16 * 64 * 4 and b.lq_grouped_workspace_bytes(16, 4, 128, 64, 1) == 0
+    assert b.lq_grouped_workspace_bytes(100_000, 4, 4096, 4096, 1) == 0 and b.lq_grouped_workspace_bytes(16, 0, 4096, 64, 1) == 0
+    assert b.lq_grouped_gradient_workspace_bytes(100_000, 4, 64, 32, 0) >= 65 * 32 * 4 and b.lq_grouped_gradient_workspace_bytes(100, 4, 64, 32, 0) == 0
     assert b.lq_adapter_workspace_bytes(8, 4, 64, 64, 4, 1) >= 8 * 8 * 4 + 8 * 4 + 256
 
 
