@@ -403,15 +403,17 @@ template <typename T, class S, class A, class B, int RING, typename F, typename 
 __device__ __forceinline__ void multiply_steps(char* lds, int steps, F&& issue, f32x4 (&acc)[S::MI][S::NI], H&& with_b) {
   constexpr int BUFFER = A::BYTES + B::BYTES, COPIES = A::PER + B::PER;
   const unsigned int at = lds_address(lds);
-  for (int step = 0; step < min(steps, RING - 1); ++step) issue(step, at + step * BUFFER);
-  int now = 0, then = RING - 1;
-  for (int step = 0; step < steps; ++step) {
+  int now = 0, then = 0;
+  for (int step = 1 - RING; step < steps; ++step) {      // (from the first copies on: issue() is in the code once)
     // this step is in LDS, and the place of the one before is read to its end
-    if (step + RING - 1 <= steps) meet_after_copies<COPIES*(RING - 2)>();
-    else meet_after_copies<0>();
+    if (step >= 0) {
+      if (step + RING - 1 <= steps) meet_after_copies<COPIES*(RING - 2)>();
+      else meet_after_copies<0>();
+    }
     if (step + RING - 1 < steps) issue(step + RING - 1, at + then * BUFFER);
+    then = then + 1 == RING ? 0 : then + 1;
+    if (step < 0) continue;
     multiply_step<T, S, A, B>(lds + now * BUFFER, lds + now * BUFFER + A::BYTES, acc, with_b);
-    then = now;
     now = now + 1 == RING ? 0 : now + 1;
   }
 }
