@@ -5,11 +5,18 @@
 // gathered and scattered through `order`) and TN columns.  How many tiles there are is known on the device only: the
 // grid holds the most there can be (n / TM and one more per group), each workgroup looks its tile up in the offsets,
 // and those past the last tile end at once.  The rows without a group get tiles too: zeros.
+// Tiles of 256 x 256 (bf16, rows aligned to 16 bytes, where they fill the compute units), 128 x 128 (from one a compute unit on), 64 x 64 (below).
+// Rows go to LDS without registers in pieces of 16 or 4 bytes; only bf16 rows of odd lengths pass through registers.
 //
 // An adapter product is ONE product over all positions with the shared W, whose inner dimension goes on: behind W's k
 // come the adapters that occur in the tile, 8 ranks at a time, with U in the rows of that adapter and zeros in the
 // others.  U is fp32; beside bf16 matrices it goes in as two bf16 numbers (its value and what that leaves), so that
-// what is lost is at most 2^-16 of it and not 2^-8.
+// what is lost is at most 2^-16 of it and not 2^-8.  Few rows take another way (AdapterPlan).
+//
+// What bounds them, measured: 8,192^3 in bf16 1,424 TFLOP/s (the vendor's dense product 1,430 on the same card), the matrix
+// instructions' power and LDS; 32,768 rows in 32 groups, 2,048 -> 4,096, 545 us = 1,010, with parts of tiles at the groups' ends; fp32
+// 8,192 x 4,096 -> 4,096 135 (vendor 150); 128 rows over 64 matrices of 2,048 x 1,024 36 to 40 us, the 268 MB of the matrices;
+// one row for two models, 1,024 -> 256, 8.4 us, 16 steps of a workgroup one after the other.
 #include "grouped.h"
 
 namespace lq {
@@ -366,8 +373,13 @@ typedef TileShape<256, 256, 2, 4, 4> Tile256;
 
 template <typename T, bool BT, int COPY, bool ADAPT> int by_size(const GroupedArgs& a, int splits, hipStream_t s) {
   const int64_t large = static_cast<int64_t>((a.n_store + 127) / 128) * ((a.n + 127) / 128);
-  if constexpr (sizeof(T) == 2 && COPY == 16)
-    if (large >= 4 * num_cus()) return launch<T, Tile256, BT, COPY, ADAPT>(a, splits, s);
+  if constexpr (sizeof(T) == 2 && COPY == 16) {
+    // One tile of 256 x 256 a compute unit at a time: where the last round of them would leave more than three in ten empty, smaller
+    // ones (16,384 rows in 16 groups, 2,048 -> 1,024, 288 tiles: 133 us, in tiles of 128 119).
+    const int64_t cus = num_cus(), half_a_tile = ADAPT ? 0 : std::min(a.n, a.G) / 2;
+    const int64_t largest = static_cast<int64_t>((a.n_store + 255) / 256) * ((a.n + 255) / 256 + half_a_tile);
+    if (largest >= cus && 10 * largest >= 7 * cus * ((largest + cus - 1) / cus)) return launch<T, Tile256, BT, COPY, ADAPT>(a, splits, s);
+  }
   // (adapters in copies of 4 bytes: the addresses of the larger tile's copies do not fit in the registers beside the rest)
   if constexpr (!(ADAPT && COPY == 4))
     if (large >= num_cus()) return launch<T, Tile128, BT, COPY, ADAPT>(a, splits, s);

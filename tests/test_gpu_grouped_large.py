@@ -15,7 +15,7 @@ def lq():
     return lq
 
 
-N, WIDE = 9_001, 2048       # 36 x 8 tiles of 256 x 256 and a part of one more for every group
+N, WIDE = 12_289, 2048      # 49 x 8 tiles of 256 x 256 and a part of one more for every group: they fill the compute units
 
 
 @pytest.mark.parametrize("transposed", [False, True], ids=["forward", "transposed"])
@@ -38,7 +38,7 @@ def test_product(lq, transposed, inner, how, out, extra):
 
 def test_rows_of_several_groups(lq):
     rng = np.random.default_rng(2)
-    G, n, slots, k = 6, 4_600, 2, 64
+    G, n, slots, k = 6, 6_200, 2, 64
     off, order = _grouping(_keys(rng, n * slots, G, "ragged"), G)
     X, W = _values(rng, (n, k), BF16, True), _values(rng, (G, k, WIDE), BF16, True)
     want, _ = _product(X, W, off, order, None, None, False, False, False, False, slots)
@@ -93,7 +93,7 @@ def test_an_adapter_of_other_rows_does_not_reach_a_row(lq):
 def test_values_within_the_bounds(lq):
     """Normal values over a long inner dimension: the tolerances of test_gpu_grouped.py."""
     rng = np.random.default_rng(4)
-    G, k, n = 3, 1000, 8_400
+    G, k, n = 3, 1000, 12_400
     off, order = _grouping(_keys(rng, n, G, "ragged"), G)
     X, W = _values(rng, (n, k), BF16, False), _values(rng, (G, k, WIDE), BF16, False)
     got = lq.lq_grouped_product(X.cuda(), W.cuda(), torch.from_numpy(off).cuda(), torch.from_numpy(order).cuda(), y_dtype=F32)
