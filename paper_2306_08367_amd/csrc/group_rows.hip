@@ -113,19 +113,36 @@ template <bool FEW> __device__ __forceinline__ void count_keys(const int32_t* __
   count_groups<FEW>(keys, G, bits, b, e, [&](int g, int n) { atomicAdd(&mine[g >> 1], static_cast<unsigned int>(n) << (16 * (g & 1))); });
 }
 
-// Turns counts per wavefront into counts of the earlier wavefronts and calls total(g, sum) for every group.
-template <typename F> __device__ __forceinline__ void sum_waves(int G, unsigned short* counts, F&& total) {
-  const int stride = 2 * count_words(G);
-  for (int g = threadIdx.x; g <= G; g += THREADS) {
-    int v[WAVES], sum = 0;
+// Turns counts per wavefront into counts of the earlier wavefronts and calls total(g, sum) for every group.  SMALL: fewer than 65,536
+// rows in all, so that two groups' sums fit in one word and are added up together.
+template <bool SMALL, typename F> __device__ __forceinline__ void sum_waves(int G, unsigned int* counts, F&& total) {
+  const int words = count_words(G);
+  if constexpr (SMALL) {
+    for (int i = threadIdx.x; i < words; i += THREADS) {
+      unsigned int v[WAVES], sum = 0;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) v[w] = counts[w * stride + g];
+      for (int w = 0; w < WAVES; ++w) v[w] = counts[w * words + i];
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      counts[w * stride + g] = static_cast<unsigned short>(sum);
-      sum += v[w];
+      for (int w = 0; w < WAVES; ++w) {
+        counts[w * words + i] = sum;
+        sum += v[w];
+      }
+      total(2 * i, static_cast<int>(sum & 0xffffu));
+      if (2 * i < G) total(2 * i + 1, static_cast<int>(sum >> 16));
     }
-    total(g, sum);
+  } else {
+    unsigned short* of = reinterpret_cast<unsigned short*>(counts);
+    for (int g = threadIdx.x; g <= G; g += THREADS) {
+      int v[WAVES], sum = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) v[w] = of[w * 2 * words + g];
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        of[w * 2 * words + g] = static_cast<unsigned short>(sum);
+        sum += v[w];
+      }
+      total(g, sum);
+    }
   }
 }
 
@@ -179,7 +196,7 @@ __global__ __launch_bounds__(THREADS) void group_rows_kernel(const int32_t* __re
   unsigned int* mine = counts + (threadIdx.x >> 6) * words;
   count_keys<false>(keys, G, bits, b, e, mine);
   __syncthreads();
-  sum_waves(G, reinterpret_cast<unsigned short*>(counts), [&](int g, int sum) { shared_base[g] = sum; });
+  sum_waves<true>(G, counts, [&](int g, int sum) { shared_base[g] = sum; });
   __syncthreads();
   int first = 0;
   for (int g0 = 0; g0 <= G; g0 += THREADS) {
@@ -247,7 +264,6 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
   __shared__ int waves[WAVES];
   const int words = count_words(G);
   unsigned int* own = reinterpret_cast<unsigned int*>(next + G + 1);
-  unsigned short* own16 = reinterpret_cast<unsigned short*>(own);
   unsigned int* mine = own + (threadIdx.x >> 6) * words;
   int* local = reinterpret_cast<int*>(own + WAVES * words);                       // SORT: first place of a group among the SORTED rows
   unsigned short* row = reinterpret_cast<unsigned short*>(local + G + 1);         // SORT: [SORTED] row - first row of them
@@ -273,7 +289,7 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
     count_keys<FEW>(keys, G, bits, b, e, mine);
     __syncthreads();
     if constexpr (SORT) {
-      sum_waves(G, own16, [&](int g, int sum) { local[g] = sum; });
+      sum_waves<true>(G, own, [&](int g, int sum) { local[g] = sum; });
       __syncthreads();
       int before_all = 0;
       for (int g0 = 0; g0 <= G; g0 += THREADS) {
@@ -297,7 +313,7 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
       __syncthreads();
       for (int g = threadIdx.x; g <= G; g += THREADS) next[g] += (g < G ? local[g + 1] : here) - local[g];
     } else {
-      sum_waves(G, own16, [](int, int) {});
+      sum_waves<false>(G, own, [](int, int) {});
       __syncthreads();
       place_rows<FEW>(keys, G, bits, b, e, next, mine,
                  [&](int64_t r, int, int place) { order[place] = static_cast<int32_t>(r); });
