@@ -4,11 +4,11 @@
 // the keys of every group per wavefront (LDS), the second puts every row at
 //   first place of the group + rows of earlier workgroups + of earlier wavefronts + of earlier steps + of earlier lanes,
 // where the lanes of one step that share a group are told apart by ballots: no atomic decides a place, so the order is the rows'
-// own.  Up to 16,384 keys are done by one workgroup in one launch; more take three launches: counts per workgroup, sums of those over
-// the workgroups, places.  There a workgroup first sorts 8,192 rows in LDS and then writes them out in that order, so that
+// own.  Up to 10,240 keys are done by one workgroup in one launch; more take three launches: counts per workgroup, sums of those over
+// the workgroups, places.  There a workgroup first sorts up to 8,192 rows in LDS and then writes them out in that order, so that
 // neighbouring lanes write neighbouring places, as long as LDS holds that beside the counts (up to about 2,900 groups).
 // A key outside [0, G) counts as group G, whose rows come last.
-// What bounds it: 64 keys 4.5 us, a launch; 6e6 keys in 2,000 groups 67 us, 52 of them in the last launch (the 48 MB that have to move take 9): the chain of LDS accesses and ballots of a step, four wavefronts a SIMD, and the barriers between the passes.
+// What bounds it: 64 keys 4.4 us, a launch; 200,000 keys in 64 groups 14 us, three; 6e6 keys in 2,000 groups 67 us, 50 of them in the last launch (the 48 MB that have to move take 9): the chain of LDS accesses and ballots of a step, four wavefronts a SIMD, and the barriers between the passes.
 // (Rows written one by one: 75; ranks of the second pass kept in registers from the first: 67 to 71, small calls slower.)
 #include "grouped.h"
 
@@ -16,7 +16,8 @@ namespace lq {
 namespace {
 
 constexpr int THREADS = 1024, WAVES = THREADS / 64;
-constexpr int64_t ONE_GROUP_KEYS = 16384;    // most keys of the one-workgroup form
+// Most keys of the one-workgroup form (16 groups: 8,192 keys 11.0 us, in three launches 12.4; 12,000 15.4 and 12.5).
+constexpr int64_t ONE_GROUP_KEYS = 10240;
 
 __device__ __forceinline__ int group_of_key(int key, int G) { return static_cast<unsigned>(key) < static_cast<unsigned>(G) ? key : G; }
 
@@ -321,11 +322,14 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
   }
 }
 
-// Keys and number of workgroups of the three-launch form: 256 workgroups (one a compute unit) unless that leaves them fewer
-// than 8,192 keys, and at most 512K keys each (16-bit counts per wavefront hold 65,535).
+// Keys and number of workgroups of the three-launch form: 256 workgroups (one a compute unit), of at least 1,024 keys (of 8,192:
+// 200,000 keys in 64 groups 20.5 us instead of 14.3, 36,080 in 16 19.7 instead of 12.3), a whole number of rounds of SORTED where
+// that is more than one, and at most 512K keys each (16-bit counts per wavefront hold 65,535).
+constexpr int LEAST = 1024;
 void split(int64_t n, int64_t* per, int* blocks) {
-  int64_t p = std::max<int64_t>(SORTED, (n + 255) / 256);
-  p = std::min<int64_t>((p + SORTED - 1) / SORTED * SORTED, 1 << 19);
+  int64_t p = (n + 255) / 256;
+  const int64_t unit = p > SORTED ? SORTED : LEAST;
+  p = std::min<int64_t>((p + unit - 1) / unit * unit, 1 << 19);
   *per = p;
   *blocks = static_cast<int>((n + p - 1) / p);
 }

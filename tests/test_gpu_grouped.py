@@ -80,6 +80,16 @@ def test_rows_of_groups(lq, n, G, how):
     np.testing.assert_array_equal(off.cpu().numpy(), np.searchsorted(np.sort(place), np.arange(G + 1)))
 
 
+@pytest.mark.parametrize("n", [10_240, 10_241, 11_265, 262_144, 262_145, 2_097_152, 2_097_153])
+@pytest.mark.parametrize("G,how", [(3, "ragged"), (300, "even"), (4096, "even")])
+def test_rows_of_groups_where_the_shares_of_workgroups_change(lq, n, G, how):
+    keys = _keys(np.random.default_rng(n - G), n, G, how)
+    off, order = lq.lq_group_rows(torch.from_numpy(keys.astype(np.int32)).cuda(), G)
+    place = np.where(keys < 0, G, keys)
+    np.testing.assert_array_equal(order.cpu().numpy(), np.argsort(place, kind="stable"))
+    np.testing.assert_array_equal(off.cpu().numpy(), np.searchsorted(np.sort(place), np.arange(G + 1)))
+
+
 def test_rows_of_groups_at_the_ends_of_the_key_type(lq):
     keys = torch.tensor([2 ** 31 - 1, -2 ** 31, 0, -1, 1, 2, 0], dtype=torch.int32, device="cuda")
     off, order = lq.lq_group_rows(keys, 2)
