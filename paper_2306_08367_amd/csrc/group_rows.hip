@@ -6,7 +6,7 @@
 // where the lanes of one step that share a group are told apart by ballots: no atomic decides a place, so the order is the rows'
 // own.  Up to 10,240 keys are done by one workgroup in one launch; more take three launches: counts per workgroup, sums of those over
 // the workgroups, places.  There a workgroup first sorts up to 8,192 rows in LDS and then writes them out in that order, so that
-// neighbouring lanes write neighbouring places, as long as LDS holds that beside the counts (up to about 2,900 groups).
+// neighbouring lanes write neighbouring places, as long as LDS holds that beside the counts (up to 3,173 groups).
 // A key outside [0, G) counts as group G, whose rows come last.
 // What bounds it: 64 keys 4.4 us, a launch; 200,000 keys in 64 groups 14 us, three; 6e6 keys in 2,000 groups 67 us, 50 of them in the last launch (the 48 MB that have to move take 9): the chain of LDS accesses and ballots of a step, four wavefronts a SIMD, and the barriers between the passes.
 // (Rows written one by one: 75; ranks of the second pass kept in registers from the first: 67 to 71, small calls slower.)
@@ -76,9 +76,10 @@ __device__ __forceinline__ int scan_threads(int v, int* shared, int* total) {
   return before + upto - v;
 }
 
-// LDS: base [G + 1] ints, then per wavefront [G + 1] 16-bit counts (a wavefront has fewer than 65,536 keys), padded to words.
-__host__ __device__ inline int count_words(int G) { return (G + 2) >> 1; }
-inline size_t place_lds(int G) { return (static_cast<size_t>(G) + 1 + static_cast<size_t>(WAVES) * count_words(G)) * 4; }
+// LDS: base [G + 1] ints, then per wavefront [G + 1] 16-bit counts, two in a word.  sum_waves and place_rows make a count that of the
+// rows of ALL wavefronts up to its own, so what a workgroup counts at a time has to stay below 65,536 rows: a round.
+__host__ __device__ constexpr int count_words(int G) { return (G + 2) >> 1; }
+constexpr size_t place_lds(int G) { return (static_cast<size_t>(G) + 1 + static_cast<size_t>(WAVES) * count_words(G)) * 4; }
 
 // Keys [begin, end) of this workgroup, run [b, e) of a wavefront.
 __device__ __forceinline__ void wave_run(int64_t begin, int64_t end, int64_t* b, int64_t* e) {
@@ -114,36 +115,21 @@ template <bool FEW> __device__ __forceinline__ void count_keys(const int32_t* __
   count_groups<FEW>(keys, G, bits, b, e, [&](int g, int n) { atomicAdd(&mine[g >> 1], static_cast<unsigned int>(n) << (16 * (g & 1))); });
 }
 
-// Turns counts per wavefront into counts of the earlier wavefronts and calls total(g, sum) for every group.  SMALL: fewer than 65,536
-// rows in all, so that two groups' sums fit in one word and are added up together.
-template <bool SMALL, typename F> __device__ __forceinline__ void sum_waves(int G, unsigned int* counts, F&& total) {
+// Turns counts per wavefront into counts of the earlier wavefronts and calls total(g, sum) for every group.  (Of a round: two groups' sums
+// fit in one word and are added up together.)
+template <typename F> __device__ __forceinline__ void sum_waves(int G, unsigned int* counts, F&& total) {
   const int words = count_words(G);
-  if constexpr (SMALL) {
-    for (int i = threadIdx.x; i < words; i += THREADS) {
-      unsigned int v[WAVES], sum = 0;
+  for (int i = threadIdx.x; i < words; i += THREADS) {
+    unsigned int v[WAVES], sum = 0;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) v[w] = counts[w * words + i];
+    for (int w = 0; w < WAVES; ++w) v[w] = counts[w * words + i];
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
-        counts[w * words + i] = sum;
-        sum += v[w];
-      }
-      total(2 * i, static_cast<int>(sum & 0xffffu));
-      if (2 * i < G) total(2 * i + 1, static_cast<int>(sum >> 16));
+    for (int w = 0; w < WAVES; ++w) {
+      counts[w * words + i] = sum;
+      sum += v[w];
     }
-  } else {
-    unsigned short* of = reinterpret_cast<unsigned short*>(counts);
-    for (int g = threadIdx.x; g <= G; g += THREADS) {
-      int v[WAVES], sum = 0;
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) v[w] = of[w * 2 * words + g];
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
-        of[w * 2 * words + g] = static_cast<unsigned short>(sum);
-        sum += v[w];
-      }
-      total(g, sum);
-    }
+    total(2 * i, static_cast<int>(sum & 0xffffu));
+    if (2 * i < G) total(2 * i + 1, static_cast<int>(sum >> 16));
   }
 }
 
@@ -197,7 +183,7 @@ __global__ __launch_bounds__(THREADS) void group_rows_kernel(const int32_t* __re
   unsigned int* mine = counts + (threadIdx.x >> 6) * words;
   count_keys<false>(keys, G, bits, b, e, mine);
   __syncthreads();
-  sum_waves<true>(G, counts, [&](int g, int sum) { shared_base[g] = sum; });
+  sum_waves(G, counts, [&](int g, int sum) { shared_base[g] = sum; });
   __syncthreads();
   int first = 0;
   for (int g0 = 0; g0 <= G; g0 += THREADS) {
@@ -255,7 +241,12 @@ __global__ __launch_bounds__(THREADS) void group_sum_kernel(int blocks, int G, i
 // LDS of the sorting form: next places [G + 1], counts per wavefront, and of SORTED rows at a time their numbers and groups in sorted
 // order and the groups' first places among them.
 constexpr int SORTED = THREADS * AHEAD;
-inline size_t sorted_lds(int G) { return place_lds(G) + (static_cast<size_t>(G) + 1) * 4 + SORTED * 4; }
+constexpr size_t SORTED_LDS = 156 * 1024;
+constexpr size_t sorted_lds(int G) { return place_lds(G) + (static_cast<size_t>(G) + 1) * 4 + SORTED * 4; }
+static_assert(sorted_lds(3173) <= SORTED_LDS && sorted_lds(3174) > SORTED_LDS, "most groups of the sorting form");
+// Rows of a round of the form that does not sort.
+constexpr int UNSORTED = 7 * SORTED;
+static_assert(ONE_GROUP_KEYS < 65536 && SORTED < 65536 && UNSORTED < 65536, "16-bit counts of a round");
 
 template <bool SORT, bool FEW>
 __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __restrict__ keys, int64_t n, int64_t per, int G, int bits,
@@ -281,8 +272,9 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
     }
     first += total;
   }
-  for (int64_t at = begin; at < end; at += SORT ? SORTED : per) {
-    const int64_t to = SORT ? min(at + SORTED, end) : end;
+  constexpr int ROUND = SORT ? SORTED : UNSORTED;
+  for (int64_t at = begin; at < end; at += ROUND) {
+    const int64_t to = min(at + ROUND, end);
     for (int i = threadIdx.x; i < WAVES * words; i += THREADS) own[i] = 0;
     __syncthreads();
     int64_t b, e;
@@ -290,7 +282,7 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
     count_keys<FEW>(keys, G, bits, b, e, mine);
     __syncthreads();
     if constexpr (SORT) {
-      sum_waves<true>(G, own, [&](int g, int sum) { local[g] = sum; });
+      sum_waves(G, own, [&](int g, int sum) { local[g] = sum; });
       __syncthreads();
       int before_all = 0;
       for (int g0 = 0; g0 <= G; g0 += THREADS) {
@@ -314,17 +306,21 @@ __global__ __launch_bounds__(THREADS) void group_place_kernel(const int32_t* __r
       __syncthreads();
       for (int g = threadIdx.x; g <= G; g += THREADS) next[g] += (g < G ? local[g + 1] : here) - local[g];
     } else {
-      sum_waves<false>(G, own, [](int, int) {});
+      sum_waves(G, own, [](int, int) {});
       __syncthreads();
       place_rows<FEW>(keys, G, bits, b, e, next, mine,
                  [&](int64_t r, int, int place) { order[place] = static_cast<int32_t>(r); });
+      __syncthreads();
+      // (the last wavefront's counts are those of the whole round by now)
+      for (int g = threadIdx.x; g <= G; g += THREADS) next[g] += (own[(WAVES - 1) * words + (g >> 1)] >> (16 * (g & 1))) & 0xffffu;
+      __syncthreads();
     }
   }
 }
 
 // Keys and number of workgroups of the three-launch form: 256 workgroups (one a compute unit), of at least 1,024 keys (of 8,192:
 // 200,000 keys in 64 groups 20.5 us instead of 14.3, 36,080 in 16 19.7 instead of 12.3), a whole number of rounds of SORTED where
-// that is more than one, and at most 512K keys each (16-bit counts per wavefront hold 65,535).
+// that is more than one, and at most 512K keys each.
 constexpr int LEAST = 1024;
 void split(int64_t n, int64_t* per, int* blocks) {
   int64_t p = (n + 255) / 256;
@@ -389,7 +385,7 @@ int launch_group_rows(const int32_t* keys, int64_t n, int32_t G, int32_t* off, i
   LQ_LAUNCH_CHECK("group_count_kernel");
   group_sum_kernel<<<G / SUM_GROUPS + 1, THREADS, 0, s>>>(blocks, G, counts, totals);
   LQ_LAUNCH_CHECK("group_sum_kernel");
-  const bool sort = sorted_lds(G) <= 156 * 1024;
+  const bool sort = sorted_lds(G) <= SORTED_LDS;
   const size_t bytes = sort ? sorted_lds(G) : lds;
   const auto kernel = few ? group_place_kernel<true, true> : sort ? group_place_kernel<true, false> : group_place_kernel<false, false>;
   if (bytes > 64 * 1024)
