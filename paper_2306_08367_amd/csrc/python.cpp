@@ -74,16 +74,16 @@ int32_t dtype_code(PyObject* o, const at::Tensor& t) {
   raise_dtype(o, "unsupported dtype %S (float32 or bfloat16)", nullptr, nullptr);
 }
 
-// A column or other typed buffer on the GPU.
+// A column or other typed buffer on the GPU, without gaps whatever its dimensions (an [n x 1] view of a wider tensor has them).
 const at::Tensor& expect(PyObject* o, at::ScalarType st, const char* dtype_name, const char* what) {
   const at::Tensor& t = tensor(o);
   if (t.scalar_type() != st) raise_dtype(o, "%s must be %s, got %S", what, dtype_name);
-  if (!t.is_cuda()) {
-    PyErr_Format(PyExc_ValueError, "%s must live on the GPU", what);
+  if (!t.is_contiguous()) {
+    PyErr_Format(PyExc_ValueError, "%s must be contiguous", what);
     throw PyErrorSet{};
   }
-  if (t.dim() == 1 && t.numel() > 1 && t.stride(0) != 1) {
-    PyErr_Format(PyExc_ValueError, "%s must be contiguous", what);
+  if (!t.is_cuda()) {
+    PyErr_Format(PyExc_ValueError, "%s must live on the GPU", what);
     throw PyErrorSet{};
   }
   return t;
@@ -854,12 +854,12 @@ lq_stack stack_on(PyObject* o, const at::Device& dev, const char* what) {
 lq_groups groups_on(PyObject* offsets, PyObject* order, int64_t n, int32_t n_groups, const at::Device& dev) {
   on(offsets, dev, "offsets");
   const at::Tensor& off = expect_i32(offsets, "offsets");
-  if (length(off) != static_cast<int64_t>(n_groups) + 1) raise(PyExc_ValueError, "offsets must have one entry more than there are groups");
+  if (length(off) != static_cast<int64_t>(n_groups) + 1 || off.numel() != off.size(0)) raise(PyExc_ValueError, "offsets must have one entry more than there are groups");
   lq_groups g{n, n_groups, static_cast<const int32_t*>(off.data_ptr()), nullptr};
   if (order != Py_None) {
     on(order, dev, "order");
     const at::Tensor& o = expect_i32(order, "order");
-    if (length(o) != n) raise(PyExc_ValueError, "order must have one entry per position");
+    if (length(o) != n || o.numel() != n) raise(PyExc_ValueError, "order must have one entry per position");
     g.order = static_cast<const int32_t*>(o.data_ptr());
   }
   return g;
