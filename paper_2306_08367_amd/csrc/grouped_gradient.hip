@@ -261,14 +261,20 @@ template <bool BF16> __global__ __launch_bounds__(256) void gradient_sum_kernel(
 // is filled, in bf16 with aligned rows.  A workgroup's share of n rows is n * tiles / workgroups that run at once (one of 512
 // threads a compute unit, else two).  At least 1,024 rows for a tile of 256 (its partial sums take as long as 800), else 256.
 struct Plan { int side; int64_t most, places; };
+// (the kernel holds it in 32 bits; tiles behind 2^32 make no difference to that)
+constexpr int64_t most_rows(int64_t n, int64_t tiles, int64_t at_once, int64_t least) {
+  const int64_t even = n * std::min(tiles, int64_t{1} << 32) / at_once;
+  return std::min<int64_t>(std::max((even + 63) / 64 * 64, least), INT32_MAX);
+}
+static_assert(most_rows(1 << 25, 1 << 14, 256, 1024) == INT32_MAX && most_rows(1 << 30, int64_t{1} << 48, 512, 256) == INT32_MAX &&
+              most_rows(32768, 32, 256, 1024) == 4096 && most_rows(0, 1, 512, 256) == 256, "rows of a chunk");
 Plan plan_of(int64_t n, int32_t G, int32_t k, int32_t l, int32_t dtype, int copy) {
   Plan p;
   p.side = dtype == LQ_BF16 && copy == 16 && k > 192 && l > 192 ? 256 : k > 64 && l > 64 ? 128 : 64;
   const int64_t tiles = static_cast<int64_t>((k + p.side - 1) / p.side) * ((l + p.side - 1) / p.side);
-  const int64_t even = n * tiles / (num_cus() * (p.side == 256 ? 1 : 2));
-  p.most = std::max<int64_t>((even + 63) / 64 * 64, dtype == LQ_BF16 && p.side == 256 ? 1024 : 256);
+  p.most = most_rows(n, tiles, num_cus() * (p.side == 256 ? 1 : 2), p.side == 256 ? 1024 : 256);
   // chunks of groups of more than one: fewer than two for every `most` rows, and fewer than one more a group
-  p.places = std::min<int64_t>(2 * n / p.most, n / p.most + G);
+  p.places = n > p.most ? std::min<int64_t>(2 * n / p.most, n / p.most + G) : 0;
   return p;
 }
 size_t place_bytes(int64_t places, int32_t k, int32_t l) { return static_cast<size_t>(places) * (static_cast<size_t>(k) + 1) * l * 4; }

@@ -1,0 +1,24 @@
+"""CPU: sizes that the grouped calls work out for the largest arguments that they take."""
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+pytestmark = pytest.mark.skipif(not os.path.exists(os.path.join(ROOT, "paper_2306_08367_amd", "liblq.so")), reason="liblq.so not built")
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2306_08367_amd import binding
+    return binding
+
+
+@pytest.mark.parametrize("dtype", [0, 1], ids=["f32", "bf16"])
+def test_a_gradient_with_more_tiles_than_workgroups_needs_no_partial_sums(b, dtype):
+    """Where one tile of a matrix keeps every compute unit busy over all rows, groups are whole: the number of rows of a chunk stays one of 32
+    bits, and the product of rows and tiles one of 64."""
+    most = 1 << 30
+    for n, k, l in [(most, most, most), (1 << 25, 1 << 20, 1024), (most, 1 << 20, 1 << 20), (1, most, most), (0, most, most)]:
+        assert b.lq_grouped_gradient_workspace_bytes(n, b.LQ_MAX_MODELS, k, l, dtype) == 0, (n, k, l)
+    # (shared out as before: 32,768 rows over 32 tiles of 256 x 256, 8 chunks and less than one more a group)
+    assert b.lq_grouped_gradient_workspace_bytes(32_768, 16, 2048, 1024, 1) == 16 * 2049 * 1024 * 4
