@@ -645,10 +645,12 @@ int launch_adapter_product(const GroupedArgs& args, const lq_stack& A, const flo
     const int copy = std::min(main_copy, low_copy);
     return halves ? few_rows<bf16_t>(m, low, p, scale, base, copy, s) : few_rows<float>(m, low, p, scale, base, copy, s);
   }
-  const int rc = halves ? product<bf16_t>(low, false, low_copy, p.u_splits, s) : product<float>(low, false, low_copy, p.u_splits, s);
-  if (rc) return rc;
   const int per = m.rp / 8;
   const int64_t pieces = static_cast<int64_t>(m.n) * per;
+  if (pieces > MOST_THREADS - 255)
+    return fail(LQ_ERR_UNSUPPORTED, "adapter product: %d rows of rank %d are more than one launch takes", m.n, m.rank);
+  const int rc = halves ? product<bf16_t>(low, false, low_copy, p.u_splits, s) : product<float>(low, false, low_copy, p.u_splits, s);
+  if (rc) return rc;
   const unsigned blocks = static_cast<unsigned>((pieces + 255) / 256);
   const float* part = static_cast<const float*>(low.Y);
   void* u = base + p.u;

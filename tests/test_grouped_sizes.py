@@ -22,3 +22,14 @@ def test_a_gradient_with_more_tiles_than_workgroups_needs_no_partial_sums(b, dty
         assert b.lq_grouped_gradient_workspace_bytes(n, b.LQ_MAX_MODELS, k, l, dtype) == 0, (n, k, l)
     # (shared out as before: 32,768 rows over 32 tiles of 256 x 256, 8 chunks and less than one more a group)
     assert b.lq_grouped_gradient_workspace_bytes(32_768, 16, 2048, 1024, 1) == 16 * 2049 * 1024 * 4
+
+
+@pytest.mark.parametrize("n,rank", [(1 << 30, 256), (1 << 28, 256), (1 << 30, 33)])
+def test_an_adapter_product_of_too_many_ranks_is_refused(b, n, rank):
+    """A thread scales eight ranks of a row, and a launch has fewer than 2^32 threads.  Refused before anything is enqueued."""
+    import ctypes
+    at = 0x10000
+    mat = lambda rows, cols: ctypes.byref(b.lq_mat(at, rows, cols, cols, 0))
+    groups, A, B = b.lq_groups(n, 2, at, None), b.lq_stack(at, 2, 1, rank, 0, rank, rank), b.lq_stack(at, 2, rank, 1, 0, 1, rank)
+    rc = b._lib.lq_adapter_product(ctypes.byref(groups), mat(n, 1), mat(1, 1), None, ctypes.byref(A), ctypes.byref(B), None, mat(n, 1), at, 1 << 50, 0, None)
+    assert rc == 6 and f"{n} rows of rank {rank}" in b.lq_last_error(), (rc, b.lq_last_error())
