@@ -10,8 +10,8 @@
 //
 // An adapter product is ONE product over all positions with the shared W, whose inner dimension goes on: behind W's k
 // come the adapters that occur in the tile, 8 ranks at a time, with U in the rows of that adapter and zeros in the
-// others.  U is fp32; beside bf16 matrices it goes in as two bf16 numbers (its value and what that leaves), so that
-// what is lost is at most 2^-16 of it and not 2^-8.  Few rows take another way (AdapterPlan).
+// others.  U is fp32; beside bf16 matrices it goes in as two bf16 numbers (two_halves), so that what is lost is at most 2^-16 of it and
+// not 2^-8.  Few rows take another way (AdapterPlan), with the same infinities and NaNs: those of the formula with U as one number.
 //
 // What bounds them, measured: 8,192^3 in bf16 1,424 TFLOP/s (the vendor's dense product 1,430 on the same card), the matrix
 // instructions' power and LDS; 32,768 rows in 32 groups, 2,048 -> 4,096, 545 us = 1,010, with parts of tiles at the groups' ends; fp32
@@ -402,6 +402,19 @@ template <typename T> int product(const GroupedArgs& a, bool transposed, int cop
   return transposed ? by_copy<T, true, false>(a, copy, splits, s) : by_copy<T, false, false>(a, copy, splits, s);
 }
 
+// A number as two of bf16, `hi` its leading bits and `lo` the rest to eight bits, both of its sign and neither zero unless the number is:
+// both meet the same row of B, and an infinity there times both is one infinity (hi rounded to nearest leaves a rest of the other
+// sign or none, a NaN; it would lose half as much, 2^-17).  So hi is cut off, and where that leaves nothing it is the next number
+// towards zero.  A number above the largest of bf16 stays finite, an infinity or a NaN is both.  (Of numbers below 2^-103
+// the rest can be too small for bf16: an infinity times them is a NaN.)
+__device__ __forceinline__ void two_halves(float u, float* hi, float* lo) {
+  const unsigned int bits = __float_as_uint(u);
+  const bool finite = __builtin_isfinite(u);
+  const unsigned int back = (bits & 0xffffu) == 0 && u != 0.f ? 0x10000u : 0u;
+  *hi = finite ? __uint_as_float((bits & 0xffff0000u) - back) : u;
+  *lo = finite ? u - *hi : u;
+}
+
 // U from the partial sums of its product: scaled, zeros behind the last rank, as two bf16 numbers beside bf16 matrices.  Eight
 // ranks of a position a thread.
 template <bool HALVES>
@@ -424,10 +437,11 @@ __global__ __launch_bounds__(256) void adapter_scale_kernel(const float* __restr
     u32x4 hi, lo;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float x = u[e >> 1][2 * (e & 1)], y = u[e >> 1][2 * (e & 1) + 1];
-      hi[e] = f32x2_to_bf16x2(x, y);
-      const float h0 = __uint_as_float(hi[e] << 16), h1 = __uint_as_float(hi[e] & 0xffff0000u);
-      lo[e] = f32x2_to_bf16x2(__builtin_isfinite(h0) ? x - h0 : 0.f, __builtin_isfinite(h1) ? y - h1 : 0.f);    // (an infinity leaves nothing)
+      float h[2], l[2];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) two_halves(u[e >> 1][2 * (e & 1) + q], &h[q], &l[q]);
+      hi[e] = f32x2_to_bf16x2(h[0], h[1]);
+      lo[e] = f32x2_to_bf16x2(l[0], l[1]);
     }
     *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(out) + id * 8) = hi;
     *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(out) + rest + id * 8) = lo;
