@@ -133,12 +133,22 @@ template <typename F> __device__ __forceinline__ void sum_waves(int G, unsigned 
   }
 }
 
+// Lanes of a wavefront read and change each other's counts: what stands before this point is seen behind it.  (LDS keeps a wavefront's
+// order, so this is no instruction.)
+__device__ __forceinline__ void wave_meets() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // put(row, group, place) for the rows of the wavefront's run, in their order; base: first places of the groups.
 template <bool FEW, typename F>
 __device__ __forceinline__ void place_rows(const int32_t* __restrict__ keys, int G, int bits, int64_t b, int64_t e, const int* base,
                                            unsigned int* mine, F&& put) {
   const int lane = threadIdx.x & 63;
-  const volatile unsigned short* mine16 = reinterpret_cast<unsigned short*>(mine);
+  auto count = [&](int g) {
+    return static_cast<int>(__hip_atomic_load(&mine[g >> 1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT) >> (16 * (g & 1)) & 0xffffu);
+  };
   for (int64_t i0 = b; i0 < e; i0 += 64 * AHEAD) {
     int key[AHEAD];
 #pragma unroll
@@ -150,22 +160,22 @@ __device__ __forceinline__ void place_rows(const int32_t* __restrict__ keys, int
       const unsigned long long some = __ballot(in);
       if (!some) break;
       const int g = in ? group_of_key(key[j], G) : -1;
-      // (LDS keeps a wavefront's order: the counts before this step, with this step's rows, and then read again)
+      // (the counts before this step, with this step's rows, and then read again)
       int earlier = 0, after = 0, before;
-      if (in) earlier = mine16[g];
-      __builtin_amdgcn_wave_barrier();
+      if (in) earlier = count(g);
+      wave_meets();
       if constexpr (FEW) {
         const unsigned long long same = same_group(g, bits, some);
         before = __popcll(same & ((1ull << lane) - 1));
         if (in && before == 0) atomicAdd(&mine[g >> 1], static_cast<unsigned int>(__popcll(same)) << (16 * (g & 1)));
       } else {
         if (in) atomicAdd(&mine[g >> 1], 1u << (16 * (g & 1)));
-        __builtin_amdgcn_wave_barrier();
-        if (in) after = mine16[g];
+        wave_meets();
+        if (in) after = count(g);
         before = lanes_before(g, bits, in && after - earlier > 1, some);
       }
       if (in) put(i, g, base[g] + earlier + before);
-      __builtin_amdgcn_wave_barrier();
+      wave_meets();
     }
   }
 }
