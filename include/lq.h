@@ -621,7 +621,7 @@ typedef struct {
  *            then LQ_ERR_FK_RANGE and the outputs stay untouched (the call waits for that check)
  *   offsets  device int32 [n_groups + 1], out
  *   order    device int32 [n], out: rows of group 0 in ascending order, of group 1, ..., then the rows
- *            without a group, ascending
+ *            without a group, ascending.  keys, offsets and order must not overlap (LQ_ERR_SHAPE)
  *   ws       lq_group_rows_workspace_bytes(n, n_groups) bytes, 256-byte aligned (NULL where that is 0;
  *            LQ_CHECK_FKS needs 256 bytes at least)
  */

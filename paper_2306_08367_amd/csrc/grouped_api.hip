@@ -47,6 +47,12 @@ int check_workspace(const void* ws, size_t ws_bytes, size_t need, const char* wh
   return LQ_OK;
 }
 
+// Whether two columns of 4-byte entries share memory.
+bool share(const int32_t* a, int64_t na, const int32_t* b, int64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + 4 * static_cast<uintptr_t>(nb) && y < x + 4 * static_cast<uintptr_t>(na);
+}
+
 int read_flag(const int32_t* flag, int32_t* value, hipStream_t s) {
   LQ_HIP_TRY(hipMemcpyAsync(value, flag, sizeof(*value), hipMemcpyDeviceToHost, s));
   LQ_HIP_TRY(hipStreamSynchronize(s));
@@ -102,9 +108,12 @@ int lq_group_rows(const int32_t* keys, int64_t n, int32_t n_groups, int32_t* off
   if (flags & ~LQ_CHECK_FKS) return fail(LQ_ERR_UNSUPPORTED, "unknown flags 0x%x", flags);
   int rc = check_workspace(ws, ws_bytes, group_rows_ws_bytes(n, n_groups), "lq_group_rows");
   if (rc) return rc;
+  if ((flags & LQ_CHECK_FKS) && n > 0 && (rc = check_workspace(ws, ws_bytes, 256, "LQ_CHECK_FKS"))) return rc;
+  // (keys are read again while order is written: changed ones would give places outside of it)
+  if (n > 0 && (share(order, n, keys, n) || share(offsets, n_groups + 1, keys, n) || share(offsets, n_groups + 1, order, n)))
+    return fail(LQ_ERR_SHAPE, "keys, offsets and order overlap");
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   if ((flags & LQ_CHECK_FKS) && n > 0) {
-    if ((rc = check_workspace(ws, ws_bytes, 256, "LQ_CHECK_FKS"))) return rc;
     int32_t bad = 0, *flag = static_cast<int32_t*>(ws);
     if ((rc = launch_check_keys(keys, n, n_groups, flag, s))) return rc;
     if ((rc = read_flag(flag, &bad, s))) return rc;

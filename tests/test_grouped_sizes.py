@@ -33,3 +33,11 @@ def test_an_adapter_product_of_too_many_ranks_is_refused(b, n, rank):
     groups, A, B = b.lq_groups(n, 2, at, None), b.lq_stack(at, 2, 1, rank, 0, rank, rank), b.lq_stack(at, 2, rank, 1, 0, 1, rank)
     rc = b._lib.lq_adapter_product(ctypes.byref(groups), mat(n, 1), mat(1, 1), None, ctypes.byref(A), ctypes.byref(B), None, mat(n, 1), at, 1 << 50, 0, None)
     assert rc == 6 and f"{n} rows of rank {rank}" in b.lq_last_error(), (rc, b.lq_last_error())
+
+
+@pytest.mark.parametrize("keys,offsets,order", [(0, 0x1000, 0), (0, 0x1000, 36), (36, 0x1000, 0), (0, 36, 0x1000), (16, 0, 0x1000), (0x1000, 0, 16), (0x1000, 36, 0)])
+def test_rows_of_groups_in_place_are_refused(b, keys, offsets, order):
+    """10 keys, 4 groups: order or offsets over the keys, which are read while these are written, or over each other (bytes from one base)."""
+    at = 0x100000
+    rc = b._lib.lq_group_rows(at + keys, 10, 4, at + offsets, at + order, None, 0, 0, None)
+    assert rc == 2 and "overlap" in b.lq_last_error(), (rc, b.lq_last_error())
