@@ -583,6 +583,9 @@ int lq_order_groups(int32_t n_group_cols, const int32_t* group_card, int32_t n_m
  * program makes once per batch and uses for every layer, forward and backward.
  * Sums are fp32 whatever the element type.  They are taken in an order that depends on the sizes of
  * the call, of the groups and on alignment, never on timing: the same call gives the same bits.
+ * No output of a call may overlap an input, the workspace or another output.  Calls whose tiles need 2^32
+ * threads or more are LQ_ERR_UNSUPPORTED: results of 2^36 elements at the earliest (most from 2^38 on: 67
+ * million rows of 4,096 columns), adapters from 2^35 ranks of all rows together on.
  * ------------------------------------------------------------------------------------- */
 #define LQ_MAX_MODELS 4096   /* most groups */
 #define LQ_MAX_RANK 256      /* widest low-rank factor */
@@ -672,7 +675,10 @@ size_t lq_grouped_gradient_workspace_bytes(int64_t n, int32_t n_groups, int32_t 
  *   X [n x k], W [k x l], A n_groups matrices [k x rank], B n_groups matrices [rank x l], all of one type;
  *   rank 1..LQ_MAX_RANK;  bias NULL or [1 x l] of that type;  scale device fp32 [n_groups] or NULL (all 1)
  *   Y [n x l], of that type (or f32 when that is bf16); must not overlap an input
- *   The products X A_g are kept in fp32.  An adapter's infinities and NaNs reach the rows of its own group only.
+ *   The products U = scale_g X A_g are fp32; in bf16 and above a few rows they go on as two bf16 numbers, at most 2^-16
+ *   of U away.  Infinities and NaNs are those of the formula with U as one number (beside infinities a U below 2^-103
+ *   may count as zero), and an adapter's reach the rows of its own group only: above a few rows, a tile of up to 256 rows
+ *   with a NaN in its results is computed again once for each adapter that has rows in it, which takes that many times as long.
  *   flags  0 or LQ_CHECK_FKS;  ws  lq_adapter_workspace_bytes(..) bytes, 256-byte aligned, required
  */
 int lq_adapter_product(const lq_groups* groups, const lq_mat* X, const lq_mat* W, const lq_mat* bias,

@@ -734,7 +734,7 @@ def lq_group_rows(keys: torch.Tensor, n_groups: int, offsets: Optional[torch.Ten
                   flags: int = 0, ws: Optional[torch.Tensor] = None, stream=None):
     """The rows of every group of a key column, a stable counting sort: (offsets int32 [n_groups + 1], order int32 [n]).
     order[offsets[g] : offsets[g + 1]] are the rows whose key is g, ascending; rows whose key is no group (negative, or n_groups
-    and more unless LQ_CHECK_FKS refuses those) come last."""
+    and more unless LQ_CHECK_FKS refuses those) come last.  keys, offsets and order must not share memory."""
     return _lqpy.group_rows(keys, n_groups, offsets, order, flags, ws, stream)
 
 

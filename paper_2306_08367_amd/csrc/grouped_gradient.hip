@@ -10,9 +10,9 @@
 // what a workgroup gets if all rows are shared out evenly (half of that: 265 instead of 221 us below, for the partial sums' way through
 // memory), but no fewer rows than are worth a workgroup.
 //
-// What bounds it, measured: 8,192^3 in bf16 1,062 TFLOP/s, both operands transposed on their way out of LDS; 32,768 rows in 16 groups,
-// 2,048 x 1,024 into fp32, 203 us = 680, of which 25 add up partial sums, and 134 MB of results; fp32, 20,001 rows in 12 groups, 100 x 64,
-// 21 us, two short launches.
+// What bounds it, measured: 8,192^3 in bf16 1,052 TFLOP/s, both operands transposed on their way out of LDS; 32,768 rows in 16 groups,
+// 2,048 x 1,024 into fp32, 196 to 203 us = 680 to 700, of which the launch that adds up partial sums takes 16, and 134 MB of results; fp32,
+// 20,001 rows in 12 groups, 100 x 64, 20 us, two short launches.
 #include "grouped.h"
 
 namespace lq {

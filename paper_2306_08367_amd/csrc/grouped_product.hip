@@ -13,9 +13,9 @@
 // others.  U is fp32; beside bf16 matrices it goes in as two bf16 numbers (two_halves), so that what is lost is at most 2^-16 of it and
 // not 2^-8.  Few rows take another way (AdapterPlan), with the same infinities and NaNs: those of the formula with U as one number.
 //
-// What bounds them, measured: 8,192^3 in bf16 1,424 TFLOP/s (the vendor's dense product 1,430 on the same card), the matrix
-// instructions' power and LDS; 32,768 rows in 32 groups, 2,048 -> 4,096, 545 us = 1,010, with parts of tiles at the groups' ends; fp32
-// 8,192 x 4,096 -> 4,096 135 (vendor 150); 128 rows over 64 matrices of 2,048 x 1,024 36 to 40 us, the 268 MB of the matrices;
+// What bounds them, measured: 8,192^3 in bf16 1,373 TFLOP/s, transposed 1,341 (the vendor's dense product 1,350 on the same card; on
+// another 1,424 and 1,430), the matrix instructions' power and LDS; 32,768 rows in 32 groups, 2,048 -> 4,096, 545 us = 1,010, with parts of tiles at the groups' ends; fp32
+// 8,192^3 136 (vendor 154); 128 rows over 64 matrices of 2,048 x 1,024 36 to 40 us, the 268 MB of the matrices;
 // one row for two models, 1,024 -> 256, 8.4 us, 16 steps of a workgroup one after the other.
 #include "grouped.h"
 
@@ -539,7 +539,8 @@ size_t split_bytes(int64_t n, int32_t N, int splits) {
   return splits < 2 ? 0 : round_up(static_cast<size_t>(n) * 4, 256) + round_up(static_cast<size_t>(splits) * n * N * 4, 256);
 }
 
-// How an adapter product runs, and what lies where in its workspace behind the first 256 bytes (kept for LQ_CHECK_FKS).
+// How an adapter product runs, and what lies where in its workspace behind the first 256 bytes (kept for LQ_CHECK_FKS).  (For 256 compute units
+// whatever the device, so that the workspace's size is the same on all.)
 //   few rows    the products of X with W and with A in one launch of tiles of 64 x 64, both in splits of the inner dimension so that
 //               there are two tiles a compute unit, then adapter_finish_kernel: where W alone has at most one tile a compute unit and
 //               the rows' own reads of B (every row reads its adapter) stay small against the caches.  64 rows of 4,096 -> 4,096 with 48
